@@ -211,7 +211,7 @@ def _run_own(s):
         if "_plan" not in s:  # what a server keeps: the layer, the cache and a workspace
             layer = [lb.LittleBitPath(U=U, V=None, h=h, g=None, l=None) for U, h in zip(s["U"], s["h"])]
             c = lb.LatentCache(s["cache"], s["r"], s["dr"])
-            n = lb.lb_latent_attention_workspace_bytes(s["q"].shape[0], s["B"], s["H"], s["r"], s["dr"], c.capacity(s["table"]))
+            n = lb.lb_latent_attention_workspace_bytes(s["q"].shape[0], s["B"], s["H"], s["r"], s["dr"])
             s["_plan"] = (c, layer, torch.empty(max(n, 256), dtype=torch.uint8, device="cuda"))
         c, layer, ws = s["_plan"]
         return lb.lb_latent_attention(s["q"], c, layer, s["Hk"], s["dv"], s["table"], s["lens"], s["cu"], s["freqs"],
