@@ -55,7 +55,7 @@
 extern "C" {
 #endif
 
-#define LB_ABI_VERSION 7
+#define LB_ABI_VERSION 8
 
 typedef enum lb_status {
   LB_OK = 0,
@@ -451,6 +451,141 @@ size_t lb_dual_svid_workspace_bytes(int64_t d_out, int64_t d_in, int64_t r, int6
 lb_status lb_dual_svid(const void* W, lb_dtype w_dtype, int64_t d_out, int64_t d_in, int64_t r, int64_t oversample,
                        int32_t iters, uint64_t seed, const lb_svid_out* out, float* W_res, void* workspace,
                        size_t workspace_bytes, hipStream_t stream);
+
+/* ---- Paged latent cache and attention ------------------------------------- */
+
+/* A fused key/value projection is one LittleBit linear with d_out =
+   Hk (d_nope + d_v): outputs [0, Hk d_nope) are the keys of Hk key heads (the
+   part without position), the others their values.  Its latent of a token
+   (lb_linear_latent) is the one vector from which all heads' keys and values
+   follow, so a cache holds per token that latent and a rotary key of d_rope
+   values that all heads share (d_rope may be 0):
+     row = [w (2 r values: path 0, path 1) | rotary key (d_rope) | zeros]
+   with lb_latent_row(r, d_rope) elements, a multiple of 32.  Rows live in
+   pages of page_size tokens: data [n_pages x page_size x row].
+
+   A batch of n_seq sequences is described by three device arrays:
+     table [n_seq x max_pages]: the pages of each sequence, in order;
+     lens [n_seq]: cached tokens of each sequence, the call's new ones included;
+     cu [n_seq + 1]: prefix sums of the call's new tokens, cu[0] = 0: token rows
+       cu[b] .. cu[b + 1] - 1 of w and q belong to sequence b, as its last
+       positions lens[b] - (cu[b + 1] - cu[b]) .. lens[b] - 1.
+   The kernels keep every access inside the buffers whatever these arrays hold:
+   lens are cut to max_pages page_size; a token without a place (before
+   position 0, past the table, or on a page outside [0, n_pages)) is not written
+   and not seen; rows behind cu[n_seq] are neither read nor written.  A place
+   named twice in one append holds parts of either token.
+   2 r + d_rope <= 1536, d_rope even and <= 256, n_pages page_size < 2^31 and
+   max_pages page_size < 2^31 (LB_ERR_SHAPE); data may be larger than 2^31
+   elements and is 16-byte aligned. */
+typedef struct lb_latent_cache {
+  void* data;
+  lb_dtype dtype;
+  int64_t n_pages, page_size, r, d_rope;
+  const int32_t* table;
+  int64_t n_seq, max_pages;
+  const int32_t* lens;
+  const int32_t* cu;
+} lb_latent_cache;
+
+/* Host, pure.  Elements of a cache row (0 for invalid arguments). */
+int64_t lb_latent_row(int64_t r, int64_t d_rope);
+
+/* Position rotation of x [T x H x d] into y (d even, <= 256): with a =
+   positions[t] freqs[i] and the pairs (i, i + d/2), i < d/2,
+     y_i = x_i cos a - x_{i+d/2} sin a,  y_{i+d/2} = x_{i+d/2} cos a + x_i sin a;
+   inverse != 0 takes -a: the transposed map, which carries gradients back.
+   Angles are formed in 64 bits, the products in fp32, rounded once.  Element
+   (t, h, i) of x is at t x_t + h x_h + i (strides in elements, >= 0), y alike;
+   y's rows must not overlap each other (LB_ERR_ARG).  y may be x with the same
+   strides; other overlaps of the spanned ranges are refused (LB_ERR_ARG).
+   positions [T] int32, freqs [d / 2] fp32 (radians a position). */
+lb_status lb_rotate(const void* x, lb_dtype dtype, int64_t T, int64_t H, int64_t d, int64_t x_t, int64_t x_h,
+                    const int32_t* positions, const float* freqs, int inverse, void* y, int64_t y_t, int64_t y_h,
+                    hipStream_t stream);
+
+/* Append the latents w [T x 2 x r] (contiguous, as lb_linear_latent writes them)
+   and rotary keys k_rope (row t at t k_rope_t, d_rope values; NULL if d_rope is
+   0), both of dtype, to the cache: each token's row is written whole, rounded
+   once to the cache's dtype, its rotary key turned by its position (freqs
+   [d_rope / 2] as for lb_rotate; NULL: stored as it is). */
+lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const void* k_rope, int64_t k_rope_t,
+                           lb_dtype dtype, int64_t T, const float* freqs, hipStream_t stream);
+
+/* Attention of T new query tokens over the paged latent cache, with the
+   up-projection absorbed (no key or value is formed):
+     q'[p][k] = sum_i U_p[g d_nope + i][k] h_p[g d_nope + i] q[i]
+     a = softmax over the cached tokens s up to the query's position of
+         scale (q' . w_s + rot(q[d_nope ..]) . rotary key_s)
+     out[i] = sum_p h_p[v] sum_k U_p[v][k] sum_s a_s w_s[p][k],  v = Hk d_nope + g d_v + i
+   with g = h / (H / Hk) the query head's key head.  q: element (t, h, i) at
+   t q_t + h q_h + i, i < d_nope + d_rope, its last d_rope values turned by the
+   query's position (freqs; NULL: taken as they are); out [T x H x d_v]
+   contiguous, in act_dtype.  A query that sees no token gets 0.  Only U and h of
+   the paths are read (of the fused layer, d_out = Hk (d_nope + d_v)).  H a
+   multiple of Hk; d_nope, d_v <= 256 (LB_ERR_SHAPE); scale finite and > 0
+   (LB_ERR_ARG).  q' enters the scores with at least 16 significant bits (24 for
+   fp32 activations), softmax statistics and sums are fp32; probabilities enter
+   the sums with 8 bits (a bf16 cache), 11 (f16), 24 (an fp32 cache, or fp32
+   activations; 22 of them on an f16 cache).
+   workspace: 256-byte aligned, >= lb_latent_attention_workspace_bytes(T, n_seq,
+   H, r, d_rope) bytes (0 for invalid sizes), no zero-fill needed; calls that may
+   run concurrently need distinct workspaces.  Repeated calls give the same bits. */
+size_t lb_latent_attention_workspace_bytes(int64_t T, int64_t n_seq, int64_t H, int64_t r, int64_t d_rope);
+lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int64_t H, int64_t Hk, int64_t d_nope,
+                              int64_t d_v, int64_t q_t, int64_t q_h, const lb_path* paths, lb_dtype scale_dtype,
+                              const lb_latent_cache* cache, const float* freqs, float scale, void* out,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Attention over expanded keys and values (what lb_linear_forward or
+   lb_linear_from_latent of the fused layer gives), of packed sequences.
+     q [Tq x H x (d_nope + d_rope)], k [Tk x Hk x d_nope], v [Tk x Hk x d_v],
+     k_rope [Tk x d_rope]: one rotary key a token, shared by all heads (rotated
+       beforehand, like q's last d_rope values; NULL if d_rope is 0)
+   all of dtype, element (t, h, i) at t *_t + h *_h + i (k_rope: t kr_t + i).
+   cu_q, cu_k [n_seq + 1] int32: prefix sums of the sequences' queries and keys,
+   both NULL for one sequence of all rows.  causal != 0: query i of n_q sees keys
+   j <= i + n_k - n_q of its sequence.  Query head h reads key head h / (H / Hk).
+   1 <= d_nope + d_rope <= 192, 1 <= d_v <= 128 (LB_ERR_SHAPE); scale finite and
+   > 0 (LB_ERR_ARG).  Rows behind cu_q[n_seq] / cu_k[n_seq] are neither read nor
+   written; accesses stay inside the buffers whatever cu_q and cu_k hold.  A
+   masked score is left out whatever its key holds, but a NaN or infinity in v may
+   reach queries of its sequence that do not see it (a zero probability is
+   multiplied with it). */
+typedef struct lb_attention {
+  const void *q, *k, *v, *k_rope;
+  lb_dtype dtype;
+  int64_t Tq, Tk, H, Hk, d_nope, d_rope, d_v;
+  int64_t q_t, q_h, k_t, k_h, v_t, v_h, kr_t;
+  const int32_t *cu_q, *cu_k;
+  int64_t n_seq;
+  int causal;
+  float scale;
+} lb_attention;
+
+/* o [Tq x H x d_v] (dtype) and, if not NULL, lse [Tq x H] fp32, the natural
+   logarithm of the sum of the exponentials of a query's scores.  A query that
+   sees no key gets o = 0, lse = -infinity.  Probabilities are rounded to dtype for
+   their product with v; scores, statistics and sums are fp32. */
+lb_status lb_attention_forward(const lb_attention* a, void* o, float* lse, hipStream_t stream);
+
+/* Gradients for d_o = dL/do [Tq x H x d_v] (contiguous, dtype): dq contiguous
+   like q; dk, dv with the given strides (rows must not overlap); dk_rope [Tk x
+   d_rope], summed over all heads (NULL if d_rope is 0); all of dtype, written,
+   not accumulated, rounded once from fp32 sums.  o and lse are the forward's.
+   P and dS are rounded to dtype for their products.  Gradients of grouped heads
+   are summed in a fixed order: repeated calls give the same bits.  No output may
+   overlap an input or another output (not checked).  workspace: 256-byte
+   aligned, >= lb_attention_backward_workspace_bytes(Tq, Tk, H, Hk, d_rope)
+   bytes (0 for invalid sizes), no zero-fill needed. */
+typedef struct lb_attention_grads {
+  void *dq, *dk, *dv, *dk_rope;
+  int64_t dk_t, dk_h, dv_t, dv_h;
+} lb_attention_grads;
+size_t lb_attention_backward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int64_t d_rope);
+lb_status lb_attention_backward(const lb_attention* a, const void* o, const float* lse, const void* d_o,
+                                const lb_attention_grads* grads, void* workspace, size_t workspace_bytes,
+                                hipStream_t stream);
 
 /* Checking path: the dense effective weight of both paths,
      W[i][j] = sum_p h_p[i] g_p[j] sum_k U_p[i][k] l_p[k] V_p[j][k]

@@ -14,7 +14,9 @@ The names follow the C ABI:
   lb_list_workspace_bytes, lb_list_init, lb_list_forward (class LittleBitList),
   lb_linear_latent, lb_latent_workspace_bytes,
   lb_linear_from_latent, lb_from_latent_workspace_bytes,
-  lb_linear_backward, lb_backward_workspace_bytes.
+  lb_linear_backward, lb_backward_workspace_bytes,
+  lb_rotate, lb_latent_row, lb_latent_append, lb_latent_attention, lb_latent_attention_workspace_bytes
+  (class LatentCache), lb_attention_forward, lb_attention_backward, lb_attention_backward_workspace_bytes.
 """
 from __future__ import annotations
 
@@ -30,7 +32,7 @@ LB_OK, LB_ERR_NULL, LB_ERR_SHAPE, LB_ERR_DTYPE, LB_ERR_ALIGN, LB_ERR_WORKSPACE, 
 LB_F32, LB_F16, LB_BF16 = 0, 1, 2
 LB_ROLE_U, LB_ROLE_V = 0, 1
 LB_KERNEL_AUTO, LB_KERNEL_DECODE, LB_KERNEL_PREFILL, LB_KERNEL_DECODE_MFMA = 0, 1, 2, 3
-ABI_VERSION = 7
+ABI_VERSION = 8
 
 
 class LittleBitError(RuntimeError):
@@ -59,6 +61,28 @@ class lb_path_train(ctypes.Structure):
 class lb_svid_out(ctypes.Structure):
     _fields_ = [("U_latent", ctypes.c_void_p), ("V_latent", ctypes.c_void_p), ("h", ctypes.c_void_p),
                 ("g", ctypes.c_void_p), ("l", ctypes.c_void_p), ("sigma", ctypes.c_void_p)]
+
+
+class lb_latent_cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int), ("n_pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int64), ("r", ctypes.c_int64), ("d_rope", ctypes.c_int64),
+                ("table", ctypes.c_void_p), ("n_seq", ctypes.c_int64), ("max_pages", ctypes.c_int64),
+                ("lens", ctypes.c_void_p), ("cu", ctypes.c_void_p)]
+
+
+class lb_attention(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_rope", ctypes.c_void_p),
+                ("dtype", ctypes.c_int), ("Tq", ctypes.c_int64), ("Tk", ctypes.c_int64), ("H", ctypes.c_int64),
+                ("Hk", ctypes.c_int64), ("d_nope", ctypes.c_int64), ("d_rope", ctypes.c_int64), ("d_v", ctypes.c_int64),
+                ("q_t", ctypes.c_int64), ("q_h", ctypes.c_int64), ("k_t", ctypes.c_int64), ("k_h", ctypes.c_int64),
+                ("v_t", ctypes.c_int64), ("v_h", ctypes.c_int64), ("kr_t", ctypes.c_int64), ("cu_q", ctypes.c_void_p),
+                ("cu_k", ctypes.c_void_p), ("n_seq", ctypes.c_int64), ("causal", ctypes.c_int),
+                ("scale", ctypes.c_float)]
+
+
+class lb_attention_grads(ctypes.Structure):
+    _fields_ = [("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p), ("dk_rope", ctypes.c_void_p),
+                ("dk_t", ctypes.c_int64), ("dk_h", ctypes.c_int64), ("dv_t", ctypes.c_int64), ("dv_h", ctypes.c_int64)]
 
 
 _lib = None
@@ -134,6 +158,25 @@ def load_library(path: str = LIB_PATH):
     lib.lb_dual_svid.restype = i32
     lib.lb_dual_svid.argtypes = [vp, i32, i64, i64, i64, i64, i32, ctypes.c_uint64, ctypes.POINTER(lb_svid_out), vp,
                                  vp, sz, vp]
+    f32 = ctypes.c_float
+    lib.lb_latent_row.restype = i64
+    lib.lb_latent_row.argtypes = [i64, i64]
+    lib.lb_rotate.restype = i32
+    lib.lb_rotate.argtypes = [vp, i32, i64, i64, i64, i64, i64, vp, vp, i32, vp, i64, i64, vp]
+    lib.lb_latent_append.restype = i32
+    lib.lb_latent_append.argtypes = [ctypes.POINTER(lb_latent_cache), vp, vp, i64, i32, i64, vp, vp]
+    lib.lb_latent_attention_workspace_bytes.restype = sz
+    lib.lb_latent_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    lib.lb_latent_attention.restype = i32
+    lib.lb_latent_attention.argtypes = [vp, i32, i64, i64, i64, i64, i64, i64, i64, ctypes.POINTER(lb_path), i32,
+                                        ctypes.POINTER(lb_latent_cache), vp, f32, vp, vp, sz, vp]
+    lib.lb_attention_forward.restype = i32
+    lib.lb_attention_forward.argtypes = [ctypes.POINTER(lb_attention), vp, vp, vp]
+    lib.lb_attention_backward_workspace_bytes.restype = sz
+    lib.lb_attention_backward_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    lib.lb_attention_backward.restype = i32
+    lib.lb_attention_backward.argtypes = [ctypes.POINTER(lb_attention), vp, vp, vp, ctypes.POINTER(lb_attention_grads),
+                                          vp, sz, vp]
     if lib.lb_abi_version() != ABI_VERSION:
         raise RuntimeError("liblittlebit.so ABI version mismatch")
     _lib = lib
@@ -506,6 +549,233 @@ def lb_linear_backward(x, dy, paths: Sequence[LittleBitPath], train: Sequence[Li
     return dx if need_dx else None
 
 
+# ----------------------------------------------------------------------------
+# paged latent cache and attention
+# ----------------------------------------------------------------------------
+def _one_device(*tensors):
+    """Every tensor on the current GPU (a launch goes to the current device's stream)."""
+    torch = _torch()
+    cur = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != cur):
+            raise ValueError(f"every tensor must be on the current GPU (cuda:{cur}), got one on {t.device}")
+
+
+def _int32(t, shape, name: str) -> int:
+    torch = _torch()
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be int32 of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return _dev_ptr(t, name)
+
+
+def _freqs(t, d: int) -> int:
+    torch = _torch()
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or tuple(t.shape) != (d // 2,):
+        raise ValueError(f"freqs must be float32 of shape ({d // 2},), got {t.dtype} {tuple(t.shape)}")
+    return _dev_ptr(t, "freqs")
+
+
+def _rows(t, name: str, dims: int = 3):
+    """(pointer, strides) of a tensor whose last dimension is contiguous."""
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    return t.data_ptr() if t.numel() else 0, t.stride()[:-1]
+
+
+def _shape(t, shape, dtype, name: str):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def lb_rotate(x, positions, freqs, inverse: bool = False, out=None, stream=None):
+    """x [T, H, d] turned by positions [T] (int32) and freqs [d / 2] (fp32 radians a position), pairs
+    (i, i + d / 2); inverse=True turns back, which is also the gradient's map.  x and out may be strided
+    (last dimension contiguous), out may be x; returns out."""
+    torch = _torch()
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _shape(out, x.shape, x.dtype, "out")
+    _one_device(x, positions, freqs, out)
+    T, H, d = x.shape
+    px, (x_t, x_h) = _rows(x, "x")
+    py, (y_t, y_h) = _rows(out, "out")
+    st = load_library().lb_rotate(px, _dtype_code(x), T, H, d, x_t, x_h, _int32(positions, (T,), "positions"),
+                                  _freqs(freqs, d), int(inverse), py, y_t, y_h, _stream(stream))
+    _check(st, "lb_rotate")
+    return out
+
+
+def lb_latent_row(r: int, d_rope: int) -> int:
+    """Elements of a paged latent cache's row: [w (2 r) | rotary key (d_rope) | zeros], a multiple of 32."""
+    return int(load_library().lb_latent_row(r, d_rope))
+
+
+@dataclass
+class LatentCache:
+    """A paged latent cache: data [n_pages, page_size, lb_latent_row(r, d_rope)] in fp32, fp16 or bf16."""
+    data: object
+    r: int
+    d_rope: int = 0
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, r: int, d_rope: int = 0, dtype=None, device="cuda"):
+        torch = _torch()
+        return cls(torch.empty((n_pages, page_size, lb_latent_row(r, d_rope)), dtype=dtype or torch.bfloat16,
+                               device=device), r, d_rope)
+
+    def _struct(self, table, lens, cu):
+        d = self.data
+        if d.dim() != 3 or d.shape[2] != lb_latent_row(self.r, self.d_rope) or d.shape[2] == 0:
+            raise ValueError("a cache's data must be [n_pages, page_size, lb_latent_row(r, d_rope)]")
+        if table.dim() != 2:
+            raise ValueError("table must be [sequences, pages]")
+        B, M = table.shape
+        return lb_latent_cache(_dev_ptr(d, "data"), _dtype_code(d), d.shape[0], d.shape[1], self.r, self.d_rope,
+                               _int32(table, (B, M), "table"), B, M, _int32(lens, (B,), "lens"),
+                               _int32(cu, (B + 1,), "cu"))
+
+
+def lb_latent_append(cache: LatentCache, w, k_rope, freqs, table, lens, cu, stream=None):
+    """Append latents w [T, 2, r] and rotary keys k_rope [T, d_rope] (None if d_rope is 0; turned by their
+    positions with freqs, or stored as they are if it is None): sequence b's tokens are rows cu[b] ..
+    cu[b + 1] - 1 and become its last positions below lens[b], on the pages table[b] names."""
+    _one_device(cache.data, w, k_rope, freqs, table, lens, cu)
+    T = w.shape[0]
+    if tuple(w.shape) != (T, 2, cache.r):
+        raise ValueError(f"w must be [T, 2, {cache.r}]")
+    kp, kt = 0, 0
+    if cache.d_rope:
+        _shape(k_rope, (T, cache.d_rope), w.dtype, "k_rope")
+        kp, (kt,) = _rows(k_rope, "k_rope", 2)
+    c = cache._struct(table, lens, cu)
+    st = load_library().lb_latent_append(ctypes.byref(c), _dev_ptr(w, "w"), kp, kt, _dtype_code(w), T,
+                                         _freqs(freqs, cache.d_rope), _stream(stream))
+    _check(st, "lb_latent_append")
+
+
+def lb_latent_attention_workspace_bytes(T: int, n_seq: int, H: int, r: int, d_rope: int) -> int:
+    return int(load_library().lb_latent_attention_workspace_bytes(T, n_seq, H, r, d_rope))
+
+
+def lb_latent_attention(q, cache: LatentCache, paths: Sequence[LittleBitPath], Hk: int, d_v: int, table, lens, cu,
+                        freqs=None, scale=None, out=None, workspace=None, stream=None):
+    """Attention of new query tokens q [T, H, d_nope + d_rope] over the paged latent cache, the up-projection
+    absorbed; the tokens are already appended (table, lens and cu as for lb_latent_append).  paths: U and h of
+    the fused layer, d_out = Hk (d_nope + d_v), keys first.  q's last d_rope values are turned by their
+    positions with freqs (None: taken as they are).  scale defaults to (d_nope + d_rope) ** -0.5; returns
+    out [T, H, d_v]."""
+    torch = _torch()
+    _one_device(q, cache.data, freqs, table, lens, cu, out, workspace, *(t for p in paths for t in (p.U, p.h)))
+    T, H, dq = q.shape
+    dn = dq - cache.d_rope
+    if dn < 0:
+        raise ValueError("q's heads are narrower than the rotary key")
+    arr, sc = _paths_struct([LittleBitPath(p.U, None, p.h, None, None) for p in paths])
+    n_out = Hk * (dn + d_v)
+    for p in paths:
+        if p.h.numel() != n_out or p.U.numel() * p.U.element_size() < lb_packed_bytes(LB_ROLE_U, n_out, cache.r):
+            raise ValueError(f"paths must be those of a layer with d_out = Hk (d_nope + d_v) = {n_out}, r = {cache.r}")
+    if out is None:
+        out = torch.empty((T, H, d_v), dtype=q.dtype, device=q.device)
+    _shape(out, (T, H, d_v), q.dtype, "out")
+    if workspace is None:
+        workspace = _scratch(lb_latent_attention_workspace_bytes(T, lens.shape[0], H, cache.r, cache.d_rope), q.device)
+    pq, (q_t, q_h) = _rows(q, "q")
+    c = cache._struct(table, lens, cu)
+    st = load_library().lb_latent_attention(
+        pq, _dtype_code(q), T, H, Hk, dn, d_v, q_t, q_h, arr, sc, ctypes.byref(c), _freqs(freqs, cache.d_rope),
+        float(dq ** -0.5 if scale is None else scale), _dev_ptr(out, "out"), _dev_ptr(workspace, "workspace"),
+        workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "lb_latent_attention")
+    return out
+
+
+def _attention_struct(q, k, v, k_rope, cu_q, cu_k, causal, scale):
+    Tq, H, dq = q.shape
+    Tk, Hk, dn = k.shape
+    d_v = v.shape[-1]
+    dr = 0 if k_rope is None else k_rope.shape[-1]
+    if dn + dr != dq:
+        raise ValueError("q's heads must be as wide as k's and k_rope's together")
+    _shape(k, (Tk, Hk, dn), q.dtype, "k")
+    _shape(v, (Tk, Hk, d_v), q.dtype, "v")
+    pq, (q_t, q_h) = _rows(q, "q")
+    pk, (k_t, k_h) = _rows(k, "k")
+    pv, (v_t, v_h) = _rows(v, "v")
+    pr, kr_t = 0, 0
+    if dr:
+        _shape(k_rope, (Tk, dr), q.dtype, "k_rope")
+        pr, (kr_t,) = _rows(k_rope, "k_rope", 2)
+    if (cu_q is None) != (cu_k is None):
+        raise ValueError("cu_q and cu_k are given together")
+    n = 0 if cu_q is None else cu_q.shape[0] - 1
+    if cu_q is not None and n < 0:
+        raise ValueError("cu_q must hold at least one value")
+    return lb_attention(pq, pk, pv, pr, _dtype_code(q), Tq, Tk, H, Hk, dn, dr, d_v, q_t, q_h, k_t, k_h, v_t, v_h, kr_t,
+                        0 if cu_q is None else _int32(cu_q, (n + 1,), "cu_q"),
+                        0 if cu_k is None else _int32(cu_k, (n + 1,), "cu_k"), n, int(causal),
+                        float(dq ** -0.5 if scale is None else scale)), (Tq, Tk, H, Hk, dn, dr, d_v)
+
+
+def lb_attention_forward(q, k, v, k_rope=None, cu_q=None, cu_k=None, causal: bool = True, scale=None, o=None, lse=None,
+                         stream=None):
+    """Attention over expanded keys and values: q [Tq, H, d_nope + d_rope], k [Tk, Hk, d_nope], v [Tk, Hk, d_v],
+    k_rope [Tk, d_rope] (one rotary key a token for all heads, or None), any strides with a contiguous last
+    dimension; cu_q, cu_k int32 prefix sums of packed sequences (None: one sequence).  scale defaults to
+    (d_nope + d_rope) ** -0.5.  Returns (o [Tq, H, d_v], lse [Tq, H] fp32)."""
+    torch = _torch()
+    _one_device(q, k, v, k_rope, cu_q, cu_k, o, lse)
+    a, (Tq, _, H, _, _, _, d_v) = _attention_struct(q, k, v, k_rope, cu_q, cu_k, causal, scale)
+    if o is None:
+        o = torch.empty((Tq, H, d_v), dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((Tq, H), dtype=torch.float32, device=q.device)
+    _shape(o, (Tq, H, d_v), q.dtype, "o")
+    _shape(lse, (Tq, H), torch.float32, "lse")
+    st = load_library().lb_attention_forward(ctypes.byref(a), _dev_ptr(o, "o"), _dev_ptr(lse, "lse"), _stream(stream))
+    _check(st, "lb_attention_forward")
+    return o, lse
+
+
+def lb_attention_backward_workspace_bytes(Tq: int, Tk: int, H: int, Hk: int, d_rope: int) -> int:
+    return int(load_library().lb_attention_backward_workspace_bytes(Tq, Tk, H, Hk, d_rope))
+
+
+def lb_attention_backward(q, k, v, k_rope, o, lse, d_o, cu_q=None, cu_k=None, causal: bool = True, scale=None, dq=None,
+                          dk=None, dv=None, dk_rope=None, workspace=None, stream=None):
+    """Gradients of lb_attention_forward for d_o [Tq, H, d_v] (contiguous); dk and dv may be strided views (the
+    two parts of the fused layer's dy).  Returns (dq, dk, dv, dk_rope) (dk_rope None without a rotary key)."""
+    torch = _torch()
+    _one_device(q, k, v, k_rope, o, lse, d_o, cu_q, cu_k, dq, dk, dv, dk_rope, workspace)
+    a, (Tq, Tk, H, Hk, dn, dr, d_v) = _attention_struct(q, k, v, k_rope, cu_q, cu_k, causal, scale)
+    new = dict(dtype=q.dtype, device=q.device)
+    dq = torch.empty((Tq, H, dn + dr), **new) if dq is None else dq
+    dk = torch.empty((Tk, Hk, dn), **new) if dk is None else dk
+    dv = torch.empty((Tk, Hk, d_v), **new) if dv is None else dv
+    if dr and dk_rope is None:
+        dk_rope = torch.empty((Tk, dr), **new)
+    for t, shape, name in ((o, (Tq, H, d_v), "o"), (d_o, (Tq, H, d_v), "d_o"), (dq, (Tq, H, dn + dr), "dq"),
+                           (dk, (Tk, Hk, dn), "dk"), (dv, (Tk, Hk, d_v), "dv")):
+        _shape(t, shape, q.dtype, name)
+    _shape(lse, (Tq, H), torch.float32, "lse")
+    if dr:
+        _shape(dk_rope, (Tk, dr), q.dtype, "dk_rope")
+    pk, (dk_t, dk_h) = _rows(dk, "dk")
+    pv, (dv_t, dv_h) = _rows(dv, "dv")
+    g = lb_attention_grads(_dev_ptr(dq, "dq"), pk, pv, _dev_ptr(dk_rope, "dk_rope") if dr else 0, dk_t, dk_h, dv_t, dv_h)
+    if workspace is None:
+        workspace = _scratch(lb_attention_backward_workspace_bytes(Tq, Tk, H, Hk, dr), q.device)
+    st = load_library().lb_attention_backward(
+        ctypes.byref(a), _dev_ptr(o, "o"), _dev_ptr(lse, "lse"), _dev_ptr(d_o, "d_o"), ctypes.byref(g),
+        _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "lb_attention_backward")
+    return dq, dk, dv, dk_rope if dr else None
+
+
 def lb_dense_reference_weight(paths: Sequence[LittleBitPath], d_in: int, d_out: int, r: int, W=None, stream=None):
     """Dense fp32 W_hat [d_out, d_in] from the packed buffers (checking path)."""
     torch = _torch()
@@ -584,5 +854,7 @@ __all__ = [
     "lb_linear_forward_many", "lb_list_workspace_bytes", "LittleBitList", "lb_latent_workspace_bytes", "lb_from_latent_workspace_bytes", "lb_linear_latent",
     "lb_linear_from_latent", "lb_path_train", "LittleBitPathTrain", "lb_backward_workspace_bytes",
     "lb_linear_backward", "lb_svid_out", "lb_dual_svid_workspace_bytes", "svid_defaults", "lb_dual_svid",
-    "littlebit_from_dense",
+    "littlebit_from_dense", "lb_rotate", "lb_latent_row", "LatentCache", "lb_latent_append",
+    "lb_latent_attention_workspace_bytes", "lb_latent_attention", "lb_attention_forward",
+    "lb_attention_backward_workspace_bytes", "lb_attention_backward",
 ]

@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liblittlebit.so")
 SOURCES = ["api.cpp", "pack.hip", "decode.hip", "decode_mma.hip", "prefill.hip", "latent_small.hip", "backward.hip",
-           "dense_ref.hip", "stream.hip", "stream_mma.hip", "svid.hip"]
+           "dense_ref.hip", "stream.hip", "stream_mma.hip", "svid.hip", "attention_api.cpp", "rotary.hip", "latent_attn.hip",
+           "attention.hip", "attention_bwd.hip"]
 # the look-up-table kernels of decode.hip and stream.hip give bit-identical
 # results only if neither contracts a multiply and an add into one fma
 # the matrix-core kernels of these files keep their accumulators in ordinary

@@ -1,0 +1,220 @@
+// Attention over expanded keys and values of packed sequences, forward.
+//
+//   S = scale (q_n k^T + q_r k_rope^T), O = softmax(S) V, lse = log sum exp S
+//
+// One pass over the keys with a running maximum and sum.  A wave owns 32 query rows as
+// the columns of 32 x 32 tiles of S^T = K Q^T: a column's softmax then stays in two
+// lanes, its factor is the lane's own for O^T = V^T P^T, and P goes from one product
+// into the next in registers.  Bound by the matrix cores (2 (dk + dv) operations a
+// pair of query and key) and, beside them, by the softmax's vector instructions.
+#include "attn.h"
+#include "attn_common.h"
+
+namespace lb {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBM = 128;  // query rows of a workgroup (4 waves x 32)
+constexpr int kBN = 64;   // keys of a step
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct FwdArgs {
+  AttnArgs a;
+  int vec;      // rows may be read 16 bytes at a time
+  int ovec;     // ... and o written four elements at a time
+  int n_tiles;  // work items per head (an upper bound)
+};
+
+// the columns [0, 16 KC) of a key row: k, then the shared rotary key
+template <int DT, int KC, int VT>
+__global__ void __launch_bounds__(kThreads, 2) attn_fwd(FwdArgs f) {
+  constexpr int KW = 16 * KC, VW = 32 * VT;
+  constexpr int KS = tile_stride<DT>(KW), VS = tile_stride<DT>(VW);
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  char* kt = smem;
+  char* vt = smem + kBN * KS;
+  const AttnArgs& a = f.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hh = lane >> 5, col = lane & 31;
+  // heads of one key head next to each other in turn, so that every XCD keeps few of them
+  const int id = blockIdx.x, hi_ = id % a.H, G = a.H / a.Hk;
+  const int kvh = hi_ % a.Hk, h = kvh * G + hi_ / a.Hk;
+  int seq, tile;
+  if (!find_tile(a.cu_q, a.n_seq, a.Tq, kBM, id / a.H, lane, seq, tile)) return;
+  int q_lo, q_hi, k_lo, k_hi;
+  seq_range(a.cu_q, seq, a.Tq, q_lo, q_hi);
+  seq_range(a.cu_k, seq, a.Tk, k_lo, k_hi);
+  const int nq = q_hi - q_lo, nk = k_hi - k_lo;
+  // the last tiles first: with a causal mask they have the most keys
+  tile = (nq + kBM - 1) / kBM - 1 - tile;
+  const int i0 = tile * kBM, off = nk - nq;
+  const int dk = a.d_nope + a.d_rope, dv = a.d_v;
+  const int i = i0 + 32 * wave + col;  // this lane's query
+  const int lim = a.causal ? min(nk - 1, i + off) : nk - 1;  // its last key
+  const int lim_lo = a.causal ? min(nk - 1, i0 + 32 * wave + off) : nk - 1;
+  const int n_end = a.causal ? min(nk, min(i0 + kBM, nq) + off) : nk;
+
+  constexpr int ES = esize<DT>();
+  const char* qp = static_cast<const char*>(a.q) + ((q_lo + min(i, nq - 1)) * a.q_t + h * a.q_h) * ES;
+  Frag<DT> qf[KC];
+#pragma unroll
+  for (int c = 0; c < KC; ++c) qf[c] = load8<DT>(qp, 16 * c + 8 * hh, dk, f.vec);
+
+  floatx16 o[VT];
+#pragma unroll
+  for (int t = 0; t < VT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
+  float mx = -INFINITY, sum = 0.0f;
+  const float sc = a.scale * kLog2e;
+
+  constexpr int KL = kBN * KW / 8 / kThreads, VL = kBN * VW / 8 / kThreads;  // groups of eight per thread
+  Frag<DT> kr[KL], vr[VL];
+  const char* kp = static_cast<const char*>(a.k) + kvh * a.k_h * ES;
+  const char* vp = static_cast<const char*>(a.v) + kvh * a.v_h * ES;
+  const char* rp = static_cast<const char*>(a.k_rope);
+  auto fetch = [&](int j0) {
+#pragma unroll
+    for (int n = 0; n < KL; ++n) {
+      const int u = tid + n * kThreads, row = u / (KW / 8), c = 8 * (u % (KW / 8));
+      const int64_t t = k_lo + j0 + row;
+      kr[n] = j0 + row < nk ? load8_joined<DT>(kp + t * a.k_t * ES, a.d_nope, rp + t * a.kr_t * ES, a.d_rope, c, f.vec)
+                            : frag_zero<DT>();
+    }
+#pragma unroll
+    for (int n = 0; n < VL; ++n) {
+      const int u = tid + n * kThreads, row = u / (VW / 8), c = 8 * (u % (VW / 8));
+      vr[n] = j0 + row < nk ? load8<DT>(vp + (k_lo + j0 + row) * a.v_t * ES, c, dv, f.vec) : frag_zero<DT>();
+    }
+  };
+  if (n_end > 0) fetch(0);
+  for (int j0 = 0; j0 < n_end; j0 += kBN) {
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < KL; ++n) {
+      const int u = tid + n * kThreads;
+      tile_put<DT>(kt, KS, u / (KW / 8), 8 * (u % (KW / 8)), kr[n]);
+    }
+#pragma unroll
+    for (int n = 0; n < VL; ++n) {
+      const int u = tid + n * kThreads;
+      tile_put<DT>(vt, VS, u / (VW / 8), 8 * (u % (VW / 8)), vr[n]);
+    }
+    __syncthreads();
+    if (j0 + kBN < n_end) fetch(j0 + kBN);
+
+    floatx16 s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) s[b] = mma32<DT>(frag_rows<DT>(kt, KS, 32 * b, 16 * c, lane), qf[c], s[b]);
+    }
+    if (j0 + kBN - 1 > lim_lo) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (j0 + 32 * b + 8 * (e >> 2) + 4 * hh + (e & 3) > lim) s[b][e] = -INFINITY;
+    }
+    float tm = s[0][0];
+#pragma unroll
+    for (int e = 1; e < 32; ++e) tm = fmaxf(tm, s[e >> 4][e & 15]);
+    tm = fmaxf(tm, __shfl_xor(tm, 32));
+    if (__any(tm > mx)) {
+      const float m2 = fmaxf(mx, tm);
+      const float r = m2 == -INFINITY ? 1.0f : exp2f((mx - m2) * sc);
+      mx = m2;
+      sum *= r;
+#pragma unroll
+      for (int t = 0; t < VT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[t][e] *= r;
+    }
+    const float mz = mx == -INFINITY ? 0.0f : mx * sc;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[b][e] = exp2f(s[b][e] * sc - mz);
+        sum += s[b][e];
+      }
+#pragma unroll
+      for (int sl = 0; sl < 2; ++sl) {
+        // the probabilities in the operands' type: one rounding each (their sum keeps 32 bits)
+        float pv[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pv[e] = s[b][8 * sl + e];
+        const Frag<DT> pf = frag_from<DT>(pv);
+#pragma unroll
+        for (int t = 0; t < VT; ++t)
+          o[t] = mma32<DT>(frag_cols<DT>(vt, VS, 32 * b + 16 * sl, 32 * t, lane), pf, o[t]);
+      }
+    }
+  }
+  sum += __shfl_xor(sum, 32);
+  if (i >= nq) return;
+  const float inv = mx == -INFINITY ? 0.0f : 1.0f / sum;
+  const int64_t row = static_cast<int64_t>(q_lo + i) * a.H + h;
+  if (a.lse != nullptr && hh == 0) a.lse[row] = mx == -INFINITY ? -INFINITY : mx * a.scale + log2f(sum) * kLn2;
+  char* op = static_cast<char*>(a.o) + row * dv * ES;
+#pragma unroll
+  for (int t = 0; t < VT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      store4<DT>(op, 32 * t + 2 * e + 4 * hh, dv, f.ovec, o[t][e] * inv, o[t][e + 1] * inv, o[t][e + 2] * inv,
+                 o[t][e + 3] * inv);
+}
+
+template <int DT, int KC, int VT>
+hipError_t fwd_launch(const FwdArgs& f, hipStream_t stream) {
+  static LdsLimit limit;
+  const size_t lds = static_cast<size_t>(kBN) * (tile_stride<DT>(16 * KC) + tile_stride<DT>(32 * VT));
+  const hipError_t e = raise_lds(reinterpret_cast<const void*>(&attn_fwd<DT, KC, VT>), lds, limit);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((attn_fwd<DT, KC, VT>), dim3(static_cast<uint32_t>(f.n_tiles) * f.a.H), dim3(kThreads), lds, stream,
+                     f);
+  return hipGetLastError();
+}
+template <int DT, int VT>
+hipError_t fwd_kc(const FwdArgs& f, hipStream_t stream) {
+  const int dk = f.a.d_nope + f.a.d_rope;
+  if (dk <= 64) return fwd_launch<DT, 4, VT>(f, stream);
+  if (dk <= 96) return fwd_launch<DT, 6, VT>(f, stream);
+  if (dk <= 128) return fwd_launch<DT, 8, VT>(f, stream);
+  return fwd_launch<DT, 12, VT>(f, stream);
+}
+template <int DT>
+hipError_t fwd_dt(const FwdArgs& f, hipStream_t stream) {
+  return f.a.d_v <= 64 ? fwd_kc<DT, 2>(f, stream) : fwd_kc<DT, 4>(f, stream);
+}
+
+}  // namespace
+
+// whether 16-byte reads fit every operand (both passes)
+bool attn_vec(const AttnArgs& a, bool backward) {
+  const int es = a.dt == kDtF32 ? 4 : 2, v = 16 / es;
+  auto ok = [&](const void* p, int64_t st, int64_t sh) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && st % v == 0 && sh % v == 0;
+  };
+  bool r = a.d_nope % 8 == 0 && a.d_rope % 8 == 0 && a.d_v % 8 == 0 && ok(a.q, a.q_t, a.q_h) && ok(a.k, a.k_t, a.k_h) &&
+           ok(a.v, a.v_t, a.v_h) && (a.d_rope == 0 || ok(a.k_rope, a.kr_t, 0));
+  if (backward) r = r && ok(a.d_o, a.d_v, a.d_v);
+  return r;
+}
+
+bool attn_supports(int64_t dk, int64_t dv) { return dk >= 1 && dk <= 192 && dv >= 1 && dv <= 128; }
+
+hipError_t launch_attn_forward(const AttnArgs& a, hipStream_t stream) {
+  FwdArgs f{a, attn_vec(a, false), reinterpret_cast<uintptr_t>(a.o) % 16 == 0 && a.d_v % 4 == 0, (a.Tq + kBM - 1) / kBM + (a.cu_q ? a.n_seq : 0)};
+  switch (a.dt) {
+    case kDtF32: return fwd_dt<kDtF32>(f, stream);
+    case kDtF16: return fwd_dt<kDtF16>(f, stream);
+    default: return fwd_dt<kDtBF16>(f, stream);
+  }
+}
+
+}  // namespace lb

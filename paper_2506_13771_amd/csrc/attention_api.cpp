@@ -1,0 +1,313 @@
+// C ABI of the paged latent cache and the attention calls: host-side validation
+// and launch.  Nothing is enqueued unless every check has passed.
+#include <cmath>
+#include <cstring>
+
+#include "attn.h"
+
+namespace {
+
+constexpr int64_t kMaxElems = (int64_t(1) << 31) - 1;
+
+template <typename E>
+int enum_value(const E& e) {
+  static_assert(sizeof(E) == sizeof(int), "enums of the ABI are int-sized");
+  int v;
+  std::memcpy(&v, &e, sizeof v);
+  return v;
+}
+bool dtype_ok(const lb_dtype& d) {
+  const int v = enum_value(d);
+  return v == LB_F32 || v == LB_F16 || v == LB_BF16;
+}
+int64_t dtype_size(lb_dtype d) { return d == LB_F32 ? 4 : 2; }
+bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// a b (and a b c) below 2^31, all factors >= 0
+bool fits(int64_t a, int64_t b) { return a == 0 || b <= kMaxElems / a; }
+bool fits(int64_t a, int64_t b, int64_t c) { return fits(a, b) && fits(a * b, c); }
+
+// A strided [T x H x d] operand: its last element's offset within 2^62, strides >= 0
+constexpr int64_t kMaxStride = int64_t(1) << 40;
+bool strides_ok(int64_t st, int64_t sh) { return st >= 0 && sh >= 0 && st <= kMaxStride && sh <= kMaxStride; }
+// elements from the first to one past the last
+int64_t span(int64_t T, int64_t H, int64_t d, int64_t st, int64_t sh) { return (T - 1) * st + (H - 1) * sh + d; }
+// rows of d elements that share no element: heads inside tokens, or tokens inside heads
+bool rows_apart(int64_t T, int64_t H, int64_t d, int64_t st, int64_t sh) {
+  if (T == 0 || H == 0 || d == 0) return true;
+  const bool heads_in = (H == 1 || sh >= d) && (T == 1 || st >= (H - 1) * sh + d);
+  const bool tokens_in = (T == 1 || st >= d) && (H == 1 || sh >= (T - 1) * st + d);
+  return heads_in || tokens_in;
+}
+bool ranges_meet(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return na > 0 && nb > 0 && x < y + static_cast<uintptr_t>(nb) && y < x + static_cast<uintptr_t>(na);
+}
+
+bool cache_sizes_ok(int64_t r, int64_t d_rope) {
+  return r >= 1 && d_rope >= 0 && d_rope % 2 == 0 && d_rope <= lb::kMaxRope && r <= lb::kMaxLatentRank &&
+         2 * r + d_rope <= lb::kMaxLatentRow;
+}
+
+lb_status check_cache(const lb_latent_cache* c) {
+  if (!c) return LB_ERR_NULL;
+  if (!dtype_ok(c->dtype)) return LB_ERR_DTYPE;
+  if (!cache_sizes_ok(c->r, c->d_rope) || c->n_pages < 0 || c->page_size < 1 || c->n_seq < 0 || c->max_pages < 0 ||
+      c->n_seq > (1 << 24) || !fits(c->n_pages, c->page_size) || !fits(c->max_pages, c->page_size) ||
+      !fits(c->n_seq, c->max_pages))
+    return LB_ERR_SHAPE;
+  return LB_OK;
+}
+// the pointers of a cache that a call with work reads
+lb_status check_cache_ptrs(const lb_latent_cache* c) {
+  if ((c->n_pages > 0 && !c->data) || (c->max_pages > 0 && c->n_seq > 0 && !c->table) || !c->lens || !c->cu)
+    return LB_ERR_NULL;
+  if (!aligned(c->data, 16) || !aligned(c->table, 4) || !aligned(c->lens, 4) || !aligned(c->cu, 4)) return LB_ERR_ALIGN;
+  return LB_OK;
+}
+lb::CacheArgs cache_args(const lb_latent_cache* c) {
+  lb::CacheArgs a{};
+  a.data = c->data;
+  a.dt = c->dtype;
+  a.n_pages = c->n_pages;
+  a.page_size = static_cast<int>(c->page_size);
+  a.r = static_cast<int>(c->r);
+  a.d_rope = static_cast<int>(c->d_rope);
+  a.row = lb::latent_row(c->r, c->d_rope);
+  a.table = c->table;
+  a.n_seq = static_cast<int>(c->n_seq);
+  a.max_pages = c->n_pages == 0 ? 0 : static_cast<int>(c->max_pages);  // no page: no token has a place
+  a.lens = c->lens;
+  a.cu = c->cu;
+  return a;
+}
+
+lb_status hip_status(hipError_t e) { return e == hipSuccess ? LB_OK : LB_ERR_HIP; }
+
+bool scale_ok(float s) { return std::isfinite(s) && s > 0.0f; }
+
+}  // namespace
+
+extern "C" {
+
+int64_t lb_latent_row(int64_t r, int64_t d_rope) { return cache_sizes_ok(r, d_rope) ? lb::latent_row(r, d_rope) : 0; }
+
+lb_status lb_rotate(const void* x, lb_dtype dtype, int64_t T, int64_t H, int64_t d, int64_t x_t, int64_t x_h,
+                    const int32_t* positions, const float* freqs, int inverse, void* y, int64_t y_t, int64_t y_h,
+                    hipStream_t stream) {
+  if (!dtype_ok(dtype)) return LB_ERR_DTYPE;
+  if (T < 0 || H < 0 || d < 0 || d % 2 != 0 || d > lb::kMaxRope || !fits(T, H, d) || !strides_ok(x_t, x_h) ||
+      !strides_ok(y_t, y_h))
+    return LB_ERR_SHAPE;
+  if (T == 0 || H == 0 || d == 0) return LB_OK;
+  if (!x || !y || !positions || !freqs) return LB_ERR_NULL;
+  const int64_t es = dtype_size(dtype);
+  if (!aligned(x, es) || !aligned(y, es) || !aligned(positions, 4) || !aligned(freqs, 4)) return LB_ERR_ALIGN;
+  if (!rows_apart(T, H, d, y_t, y_h)) return LB_ERR_ARG;
+  const bool in_place = x == y && (T == 1 || x_t == y_t) && (H == 1 || x_h == y_h);
+  if (!in_place && ranges_meet(x, span(T, H, d, x_t, x_h) * es, y, span(T, H, d, y_t, y_h) * es)) return LB_ERR_ARG;
+  lb::RotateArgs a{};
+  a.x = x, a.y = y;
+  a.dt = dtype;
+  a.T = static_cast<int>(T), a.H = static_cast<int>(H), a.d = static_cast<int>(d);
+  a.x_t = x_t, a.x_h = x_h, a.y_t = y_t, a.y_h = y_h;
+  a.positions = positions, a.freqs = freqs;
+  a.inverse = inverse != 0;
+  return hip_status(lb::launch_rotate(a, stream));
+}
+
+lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const void* k_rope, int64_t k_rope_t,
+                           lb_dtype dtype, int64_t T, const float* freqs, hipStream_t stream) {
+  if (!dtype_ok(dtype)) return LB_ERR_DTYPE;
+  lb_status st = check_cache(cache);
+  if (st != LB_OK) return st;
+  if (T < 0 || !fits(T, lb::latent_row(cache->r, cache->d_rope)) || !strides_ok(k_rope_t, 0)) return LB_ERR_SHAPE;
+  if (T == 0 || cache->n_seq == 0) return LB_OK;
+  if (!w || (cache->d_rope > 0 && !k_rope)) return LB_ERR_NULL;
+  st = check_cache_ptrs(cache);
+  if (st != LB_OK) return st;
+  const int64_t es = dtype_size(dtype);
+  if (!aligned(w, es) || !aligned(k_rope, es) || !aligned(freqs, 4)) return LB_ERR_ALIGN;
+  const lb::CacheArgs c = cache_args(cache);
+  const int64_t nc = cache->n_pages * cache->page_size * c.row * dtype_size(cache->dtype);
+  if (ranges_meet(cache->data, nc, w, T * 2 * cache->r * es) ||
+      (cache->d_rope > 0 && ranges_meet(cache->data, nc, k_rope, span(T, 1, cache->d_rope, k_rope_t, 0) * es)))
+    return LB_ERR_ARG;
+  lb::AppendArgs a{};
+  a.c = c;
+  a.w = w, a.k_rope = k_rope;
+  a.kr_t = k_rope_t;
+  a.dt = dtype;
+  a.T = static_cast<int>(T);
+  a.freqs = freqs;
+  return hip_status(lb::launch_append(a, stream));
+}
+
+size_t lb_latent_attention_workspace_bytes(int64_t T, int64_t n_seq, int64_t H, int64_t r, int64_t d_rope) {
+  if (T < 0 || n_seq < 0 || n_seq > (1 << 24) || H < 0 || !cache_sizes_ok(r, d_rope) ||
+      !fits(T, H, lb::latent_row(r, d_rope)))
+    return 0;
+  return lb::latent_attn_workspace_bytes(static_cast<int>(T), static_cast<int>(n_seq), static_cast<int>(H),
+                                         static_cast<int>(r), static_cast<int>(d_rope));
+}
+
+lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int64_t H, int64_t Hk, int64_t d_nope,
+                              int64_t d_v, int64_t q_t, int64_t q_h, const lb_path* paths, lb_dtype scale_dtype,
+                              const lb_latent_cache* cache, const float* freqs, float scale, void* out,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (!dtype_ok(act_dtype) || !dtype_ok(scale_dtype)) return LB_ERR_DTYPE;
+  lb_status st = check_cache(cache);
+  if (st != LB_OK) return st;
+  if (T < 0 || H < 0 || Hk < 1 || H % Hk != 0 || d_nope < 0 || d_nope > 256 || d_v < 0 || d_v > 256 ||
+      !strides_ok(q_t, q_h) || !fits(T, H, lb::latent_row(cache->r, cache->d_rope)) ||
+      !fits(T, H, d_nope + cache->d_rope) || !fits(T, H, d_v) || !fits(Hk, d_nope + d_v, cache->r))
+    return LB_ERR_SHAPE;
+  if (!scale_ok(scale)) return LB_ERR_ARG;
+  if (T == 0 || H == 0 || d_v == 0 || cache->n_seq == 0) return LB_OK;
+  if (!out || (d_nope + cache->d_rope > 0 && !q)) return LB_ERR_NULL;
+  const int64_t es = dtype_size(act_dtype), ss = dtype_size(scale_dtype);
+  if (!aligned(q, es) || !aligned(out, es) || !aligned(freqs, 4)) return LB_ERR_ALIGN;
+  if (!paths) return LB_ERR_NULL;
+  for (int p = 0; p < 2; ++p) {
+    if (!paths[p].U || !paths[p].h) return LB_ERR_NULL;
+    if (!aligned(paths[p].U, 4) || !aligned(paths[p].h, ss)) return LB_ERR_ALIGN;
+  }
+  st = check_cache_ptrs(cache);
+  if (st != LB_OK) return st;
+  if (ranges_meet(out, T * H * d_v * es, q, span(T, H, d_nope + cache->d_rope, q_t, q_h) * es)) return LB_ERR_ARG;
+  const size_t need = lb_latent_attention_workspace_bytes(T, cache->n_seq, H, cache->r, cache->d_rope);
+  if (!workspace) return LB_ERR_NULL;
+  if (!aligned(workspace, 256)) return LB_ERR_ALIGN;
+  if (workspace_bytes < need) return LB_ERR_WORKSPACE;
+  lb::LatentAttnArgs a{};
+  a.c = cache_args(cache);
+  a.q = q;
+  a.dt = act_dtype;
+  a.T = static_cast<int>(T), a.H = static_cast<int>(H), a.Hk = static_cast<int>(Hk);
+  a.d_nope = static_cast<int>(d_nope), a.d_v = static_cast<int>(d_v);
+  a.q_t = q_t, a.q_h = q_h;
+  for (int p = 0; p < 2; ++p) a.U[p] = paths[p].U, a.h[p] = paths[p].h;
+  a.sc_dt = scale_dtype;
+  a.freqs = freqs;
+  a.scale = scale;
+  a.out = out;
+  a.ws = workspace;
+  return hip_status(lb::launch_latent_attn(a, stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+lb_status check_attention(const lb_attention* a) {
+  if (!a) return LB_ERR_NULL;
+  if (!dtype_ok(a->dtype)) return LB_ERR_DTYPE;
+  if (a->Tq < 0 || a->Tk < 0 || a->H < 0 || a->Hk < 1 || a->H % a->Hk != 0 || a->d_nope < 0 || a->d_rope < 0 ||
+      a->d_nope > 192 || a->d_rope > 192 || !lb::attn_supports(a->d_nope + a->d_rope, a->d_v) || a->n_seq < 0 ||
+      a->n_seq > (1 << 24) || !strides_ok(a->q_t, a->q_h) || !strides_ok(a->k_t, a->k_h) ||
+      !strides_ok(a->v_t, a->v_h) || !strides_ok(a->kr_t, 0))
+    return LB_ERR_SHAPE;
+  const int64_t dk = a->d_nope + a->d_rope;
+  if (!fits(a->Tq, a->H, dk) || !fits(a->Tq, a->H, a->d_v) || !fits(a->Tk, a->Hk, dk) || !fits(a->Tk, a->Hk, a->d_v) ||
+      !fits(a->n_seq + 1, a->H))
+    return LB_ERR_SHAPE;
+  if ((a->cu_q == nullptr) != (a->cu_k == nullptr) || !scale_ok(a->scale)) return LB_ERR_ARG;
+  return LB_OK;
+}
+lb_status check_attention_ptrs(const lb_attention* a) {
+  if (a->Tq > 0 && a->H > 0 && !a->q) return LB_ERR_NULL;
+  if (a->Tk > 0 && ((a->d_nope > 0 && !a->k) || !a->v || (a->d_rope > 0 && !a->k_rope))) return LB_ERR_NULL;
+  const int64_t es = dtype_size(a->dtype);
+  if (!aligned(a->q, es) || !aligned(a->k, es) || !aligned(a->v, es) || !aligned(a->k_rope, es) ||
+      !aligned(a->cu_q, 4) || !aligned(a->cu_k, 4))
+    return LB_ERR_ALIGN;
+  return LB_OK;
+}
+lb::AttnArgs attention_args(const lb_attention* a) {
+  lb::AttnArgs r{};
+  r.q = a->q, r.k = a->k, r.v = a->v, r.k_rope = a->k_rope;
+  r.dt = a->dtype;
+  r.Tq = static_cast<int>(a->Tq), r.Tk = static_cast<int>(a->Tk);
+  r.H = static_cast<int>(a->H), r.Hk = static_cast<int>(a->Hk);
+  r.d_nope = static_cast<int>(a->d_nope), r.d_rope = static_cast<int>(a->d_rope), r.d_v = static_cast<int>(a->d_v);
+  r.q_t = a->q_t, r.q_h = a->q_h, r.k_t = a->k_t, r.k_h = a->k_h, r.v_t = a->v_t, r.v_h = a->v_h, r.kr_t = a->kr_t;
+  r.cu_q = a->cu_q, r.cu_k = a->cu_k;
+  r.n_seq = static_cast<int>(a->n_seq);
+  r.causal = a->causal != 0;
+  r.scale = a->scale;
+  return r;
+}
+
+size_t up256(int64_t n) { return static_cast<size_t>((n + 255) / 256 * 256); }
+
+}  // namespace
+
+extern "C" {
+
+lb_status lb_attention_forward(const lb_attention* a, void* o, float* lse, hipStream_t stream) {
+  lb_status st = check_attention(a);
+  if (st != LB_OK) return st;
+  if (a->Tq == 0 || a->H == 0 || (a->cu_q && a->n_seq == 0)) return LB_OK;
+  st = check_attention_ptrs(a);
+  if (st != LB_OK) return st;
+  if (!o) return LB_ERR_NULL;
+  const int64_t es = dtype_size(a->dtype);
+  if (!aligned(o, es) || !aligned(lse, 4)) return LB_ERR_ALIGN;
+  const int64_t no = a->Tq * a->H * a->d_v * es, nl = lse ? a->Tq * a->H * 4 : 0;
+  const int64_t dk = a->d_nope + a->d_rope;
+  auto meets = [&](const void* p, int64_t n) { return ranges_meet(o, no, p, n) || ranges_meet(lse, nl, p, n); };
+  if (ranges_meet(o, no, lse, nl) || meets(a->q, span(a->Tq, a->H, dk, a->q_t, a->q_h) * es) ||
+      (a->Tk > 0 && (meets(a->k, a->d_nope ? span(a->Tk, a->Hk, a->d_nope, a->k_t, a->k_h) * es : 0) ||
+                     meets(a->v, span(a->Tk, a->Hk, a->d_v, a->v_t, a->v_h) * es) ||
+                     meets(a->k_rope, a->d_rope ? span(a->Tk, 1, a->d_rope, a->kr_t, 0) * es : 0))))
+    return LB_ERR_ARG;
+  lb::AttnArgs r = attention_args(a);
+  r.o = o, r.lse = lse;
+  return hip_status(lb::launch_attn_forward(r, stream));
+}
+
+size_t lb_attention_backward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int64_t d_rope) {
+  if (Tq < 0 || Tk < 0 || H < 0 || Hk < 1 || H % Hk != 0 || d_rope < 0 || d_rope > 192 || !fits(Tq, H) ||
+      !fits(Tk, Hk, d_rope))
+    return 0;
+  return 256 + up256(Tq * H * 4) + up256(Tk * Hk * d_rope * 4);
+}
+
+lb_status lb_attention_backward(const lb_attention* a, const void* o, const float* lse, const void* d_o,
+                                const lb_attention_grads* grads, void* workspace, size_t workspace_bytes,
+                                hipStream_t stream) {
+  lb_status st = check_attention(a);
+  if (st != LB_OK) return st;
+  if (!grads) return LB_ERR_NULL;
+  if (!strides_ok(grads->dk_t, grads->dk_h) || !strides_ok(grads->dv_t, grads->dv_h)) return LB_ERR_SHAPE;
+  if (a->H == 0 || (a->Tq == 0 && a->Tk == 0) || (a->cu_q && a->n_seq == 0)) return LB_OK;
+  st = check_attention_ptrs(a);
+  if (st != LB_OK) return st;
+  if (a->Tq > 0 && (!o || !lse || !d_o || !grads->dq)) return LB_ERR_NULL;
+  if (a->Tk > 0 && ((a->d_nope > 0 && !grads->dk) || !grads->dv || (a->d_rope > 0 && !grads->dk_rope)))
+    return LB_ERR_NULL;
+  const int64_t es = dtype_size(a->dtype);
+  if (!aligned(o, es) || !aligned(lse, 4) || !aligned(d_o, es) || !aligned(grads->dq, es) || !aligned(grads->dk, es) ||
+      !aligned(grads->dv, es) || !aligned(grads->dk_rope, es))
+    return LB_ERR_ALIGN;
+  if (!rows_apart(a->Tk, a->Hk, a->d_nope, grads->dk_t, grads->dk_h) ||
+      !rows_apart(a->Tk, a->Hk, a->d_v, grads->dv_t, grads->dv_h))
+    return LB_ERR_ARG;
+  const size_t need = lb_attention_backward_workspace_bytes(a->Tq, a->Tk, a->H, a->Hk, a->d_rope);
+  if (!workspace) return LB_ERR_NULL;
+  if (!aligned(workspace, 256)) return LB_ERR_ALIGN;
+  if (workspace_bytes < need) return LB_ERR_WORKSPACE;
+  lb::AttnArgs r = attention_args(a);
+  r.o = const_cast<void*>(o);
+  r.lse = const_cast<float*>(lse);
+  r.d_o = d_o;
+  r.dq = grads->dq, r.dk = grads->dk, r.dv = grads->dv, r.dkr = grads->dk_rope;
+  r.dk_t = grads->dk_t, r.dk_h = grads->dk_h, r.dv_t = grads->dv_t, r.dv_h = grads->dv_h;
+  char* ws = static_cast<char*>(workspace);
+  r.top = reinterpret_cast<float*>(ws);
+  r.delta = reinterpret_cast<float*>(ws + 256);
+  r.dkr_part = reinterpret_cast<float*>(ws + 256 + up256(a->Tq * a->H * 4));
+  return hip_status(lb::launch_attn_backward(r, stream));
+}
+
+}  // extern "C"

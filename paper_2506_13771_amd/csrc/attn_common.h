@@ -1,0 +1,276 @@
+// Device helpers of the attention kernels: fragments of eight elements, matrix-
+// core products on 32 x 32 tiles in the operands' own type, LDS tiles with rows
+// that serve row-wise and transposed reads, and the work maps of packed sequences.
+//
+// Fragment convention (v_mfma_f32_32x32x16 and its fp32 form): lane l holds row
+// (A) or column (B) l % 32 and the eight reduction slots 8 (l / 32) .. + 7 of a
+// 16-wide slice; accumulator element e of lane l is row 8 (e / 4) + 4 (l / 32) +
+// e % 4 of column l % 32.  An accumulator's elements 8 i .. 8 i + 7 are therefore a
+// B operand over rows 16 i .. 16 i + 15 whose slot 4 a + b of lane half u stands for row
+// 16 i + 8 a + 4 u + b; frag_cols() reads the A operand with the same relabelling, so
+// probabilities go from one product into the next without leaving their registers.
+#pragma once
+#include "device_common.h"
+
+namespace lb {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <int DT>
+constexpr int esize() {
+  return DT == kDtF32 ? 4 : 2;
+}
+
+// eight elements in type DT
+template <int DT>
+struct Frag {
+  u32x4 v[DT == kDtF32 ? 2 : 1];
+};
+
+template <int DT>
+__device__ __forceinline__ Frag<DT> frag_zero() {
+  Frag<DT> f;
+#pragma unroll
+  for (int i = 0; i < (DT == kDtF32 ? 2 : 1); ++i) f.v[i] = u32x4{0u, 0u, 0u, 0u};
+  return f;
+}
+
+template <int DT>
+__device__ __forceinline__ float frag_elem(const Frag<DT>& f, int e) {
+  if constexpr (DT == kDtF32)
+    return __uint_as_float(f.v[e >> 2][e & 3]);
+  else
+    return bits_to_f32<DT>((f.v[0][e >> 1] >> (16 * (e & 1))) & 0xffffu);
+}
+
+// two fp32 values as a pair of 16-bit ones, each rounded to nearest even
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (DT == kDtBF16) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
+  } else {
+    // the fp32 values are formed first (see st in device_common.h)
+    asm volatile("" : "+v"(a), "+v"(b));
+    return static_cast<uint32_t>(__half_as_ushort(__float2half_rn(a))) |
+           (static_cast<uint32_t>(__half_as_ushort(__float2half_rn(b))) << 16);
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ Frag<DT> frag_from(const float (&x)[8]) {
+  Frag<DT> f;
+  if constexpr (DT == kDtF32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e >> 2][e & 3] = __float_as_uint(x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.v[0][e] = pack2<DT>(x[2 * e], x[2 * e + 1]);
+  }
+  return f;
+}
+
+template <int DT>
+__device__ __forceinline__ floatx16 mma32(const Frag<DT>& a, const Frag<DT>& b, floatx16 c) {
+  if constexpr (DT == kDtBF16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.v[0]),
+                                                   __builtin_bit_cast(bf16x8, b.v[0]), c, 0, 0, 0);
+  } else if constexpr (DT == kDtF16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a.v[0]),
+                                                  __builtin_bit_cast(f16x8, b.v[0]), c, 0, 0, 0);
+  } else {
+    // fp32 operands: eight products of two slots each (slot j of both lane halves)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.v[j >> 2][j & 3]),
+                                               __uint_as_float(b.v[j >> 2][j & 3]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// Eight elements at p[col .. col + 7] of a row with n elements; zero from n on.
+// vec: the row starts on a 16-byte boundary and n is a multiple of a 16-byte group.
+template <int DT>
+__device__ __forceinline__ Frag<DT> load8(const void* row, int col, int n, bool vec) {
+  Frag<DT> f = frag_zero<DT>();
+  if (vec) {
+    if constexpr (DT == kDtF32) {
+      if (col < n) f.v[0] = *reinterpret_cast<const u32x4*>(static_cast<const float*>(row) + col);
+      if (col + 4 < n) f.v[1] = *reinterpret_cast<const u32x4*>(static_cast<const float*>(row) + col + 4);
+    } else {
+      if (col < n) f.v[0] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(row) + col);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (col + e < n) {
+        const uint32_t u = ld_bits<DT>(row, col + e);
+        if constexpr (DT == kDtF32)
+          f.v[e >> 2][e & 3] = u;
+        else
+          f.v[0][e >> 1] |= u << (16 * (e & 1));
+      }
+    }
+  }
+  return f;
+}
+// the same over two joined parts: columns [0, n0) of r0, then [n0, n0 + n1) of r1
+template <int DT>
+__device__ __forceinline__ Frag<DT> load8_joined(const void* r0, int n0, const void* r1, int n1, int col, bool vec) {
+  if (vec) return col < n0 ? load8<DT>(r0, col, n0, true) : load8<DT>(r1, col - n0, n1, true);
+  if (col + 8 <= n0 || n1 == 0) return load8<DT>(r0, col, n0, false);
+  if (col >= n0) return load8<DT>(r1, col - n0, n1, false);
+  Frag<DT> f = load8<DT>(r0, col, n0, false);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int c = col + e - n0;
+    if (c >= 0 && c < n1) {
+      const uint32_t u = ld_bits<DT>(r1, c);
+      if constexpr (DT == kDtF32)
+        f.v[e >> 2][e & 3] = u;
+      else
+        f.v[0][e >> 1] |= u << (16 * (e & 1));
+    }
+  }
+  return f;
+}
+
+// four values at row[col ..] of a row with n elements, rounded once; vec: as one store
+// (col a multiple of 4, so is n, the row aligned to four elements)
+template <int DT>
+__device__ __forceinline__ void store4(void* row, int col, int n, bool vec, float v0, float v1, float v2, float v3) {
+  char* p = static_cast<char*>(row) + col * esize<DT>();
+  if (vec) {
+    if (col >= n) return;
+    if constexpr (DT == kDtF32)
+      *reinterpret_cast<float4*>(p) = make_float4(v0, v1, v2, v3);
+    else
+      *reinterpret_cast<u32x2*>(p) = u32x2{pack2<DT>(v0, v1), pack2<DT>(v2, v3)};
+  } else {
+    if (col < n) st<DT>(p, 0, v0);
+    if (col + 1 < n) st<DT>(p, 1, v1);
+    if (col + 2 < n) st<DT>(p, 2, v2);
+    if (col + 3 < n) st<DT>(p, 3, v3);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// LDS tiles: rows of W elements, the row stride a number of 16-byte slots that is 3,
+// 5, 11 or 13 modulo 16.  Row-wise reads (16 rows at one slot) then meet 16 different
+// slots of the 64 banks, transposed reads (8 rows of 4 slots) at most 3 in one slot
+// where 2 is the least.
+// ---------------------------------------------------------------------------
+template <int DT>
+constexpr int tile_stride(int W) {  // bytes
+  int s = W * esize<DT>() / 16;
+  while (!(s % 16 == 3 || s % 16 == 5 || s % 16 == 11 || s % 16 == 13)) ++s;
+  return 16 * s;
+}
+
+template <int DT>
+__device__ __forceinline__ void tile_put(char* t, int stride, int row, int col, const Frag<DT>& f) {
+  char* p = t + row * stride + col * esize<DT>();
+  *reinterpret_cast<u32x4*>(p) = f.v[0];
+  if constexpr (DT == kDtF32) *reinterpret_cast<u32x4*>(p + 16) = f.v[1];
+}
+
+// A or B operand from rows: lane l takes row row0 + l % 32, columns col + 8 (l / 32) .. + 7
+template <int DT>
+__device__ __forceinline__ Frag<DT> frag_rows(const char* t, int stride, int row0, int col, int lane) {
+  const char* p = t + (row0 + (lane & 31)) * stride + (col + 8 * (lane >> 5)) * esize<DT>();
+  Frag<DT> f;
+  f.v[0] = *reinterpret_cast<const u32x4*>(p);
+  if constexpr (DT == kDtF32) f.v[1] = *reinterpret_cast<const u32x4*>(p + 16);
+  return f;
+}
+
+// A operand from columns: lane l takes column col + l % 32 at rows row0 + 8 a + 4 (l / 32)
+// + b (slot 4 a + b).  16-bit types: two transposed reads (each 16-lane group takes
+// 4 rows x 16 columns).
+template <int DT>
+__device__ __forceinline__ Frag<DT> frag_cols(const char* t, int stride, int row0, int col, int lane) {
+  Frag<DT> f;
+  const int u = lane >> 5;
+  if constexpr (DT == kDtF32) {
+    const char* p = t + (row0 + 4 * u) * stride + (col + (lane & 31)) * 4;
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      f.v[s >> 2][s & 3] = *reinterpret_cast<const uint32_t*>(p + (8 * (s >> 2) + (s & 3)) * stride);
+  } else {
+    typedef __attribute__((address_space(3))) s16x4* lds4;
+    const int i = lane & 15, c = col + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
+    const char* p = t + (row0 + 4 * u + (i >> 2)) * stride + c * 2;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 8 * stride));
+    const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+    f.v[0] = u32x4{a[0], a[1], b[0], b[1]};
+  }
+  return f;
+}
+
+// ---------------------------------------------------------------------------
+// packed sequences
+// ---------------------------------------------------------------------------
+// Sequence b's rows [lo, hi) by its prefix sums, kept inside [0, T) whatever they hold
+// (cu == nullptr: one sequence of all T rows).
+__device__ __forceinline__ void seq_range(const int32_t* cu, int b, int T, int& lo, int& hi) {
+  if (cu == nullptr) {
+    lo = 0, hi = T;
+    return;
+  }
+  lo = min(max(cu[b], 0), T);
+  hi = min(max(cu[b + 1], lo), T);
+}
+
+// The sequence and the tile of `rows` rows in it that work item `item` stands for
+// (every sequence has ceil(n / rows) tiles); false if there are fewer items.  Called by
+// whole waves: 64 sequences a step.
+__device__ __forceinline__ bool find_tile(const int32_t* cu, int n_seq, int T, int rows, int item, int lane, int& seq,
+                                          int& tile) {
+  if (cu == nullptr) {
+    seq = 0, tile = item;
+    return item < (T + rows - 1) / rows;
+  }
+  int before = 0;
+  for (int b0 = 0; b0 < n_seq; b0 += 64) {
+    const int b = b0 + lane;
+    int n = 0;
+    if (b < n_seq) {
+      int lo, hi;
+      seq_range(cu, b, T, lo, hi);
+      n = (hi - lo + rows - 1) / rows;
+    }
+    int incl = n;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int o = __shfl_up(incl, s);
+      if (lane >= s) incl += o;
+    }
+    const uint64_t m = __ballot(before + incl > item);
+    if (m != 0) {
+      const int w = __builtin_ctzll(m);
+      seq = b0 + w;
+      tile = item - before - (__shfl(incl, w) - __shfl(n, w));
+      return true;
+    }
+    before += __shfl(incl, 63);
+  }
+  return false;
+}
+
+// ---------------------------------------------------------------------------
+// position rotation
+// ---------------------------------------------------------------------------
+// cos and sin of position * frequency.  The angle is formed and brought to one turn in
+// 64 bits (exact to 2^-21 of a turn's last fp32 place at positions up to 2^31), the
+// functions are taken in fp32 of the remaining half turn.
+__device__ __forceinline__ void turn_of(int position, float freq, float& c, float& s) {
+  const double t = static_cast<double>(position) * static_cast<double>(freq) * 0.15915494309189533577;
+  const float f = static_cast<float>(t - rint(t));  // turns, in [-1/2, 1/2]
+  sincospif(2.0f * f, &s, &c);
+}
+
+}  // namespace lb

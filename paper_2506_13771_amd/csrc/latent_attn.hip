@@ -1,0 +1,790 @@
+// Attention read from the paged latent cache, the up-projection absorbed.
+//
+// A token's keys and values are K = U_k w and V = U_v w of its one latent w (2 r
+// values), so with q' = U_k^T (h_k (.) q) the scores are q' . w + q_rope . k_rope and
+// the output is h_v (.) U_v (sum_t a_t w_t): every query head reads the same cache
+// rows, once, and nothing is expanded.  Three launches:
+//
+//   absorb   q' of every (token, head), with the rotated rotary part behind it and the
+//            softmax scale folded into a factor per row, cut into terms of the cache's
+//            type: TQ terms, so that q' (not a value of that type) enters the scores
+//            with 16 bits or more.
+//   split    the cache in one pass with a running maximum and sum.  A workgroup takes
+//            an equal share of all sequences' tiles, whatever their lengths.
+//   join     the partial results of a row joined, then h (.) U_v of the sum.
+//
+// split is bound by the cache's bytes: a row of 2 r + d_rope values serves 32 query
+// rows (a model's heads) as the columns of 32 x 32 matrix-core tiles.
+#include "attn.h"
+#include "attn_common.h"
+
+namespace lb {
+
+namespace {
+
+typedef __attribute__((address_space(3))) void* lds_ptr;
+typedef __attribute__((address_space(1))) const void* glb_ptr;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr size_t kLdsMax = 163840;
+constexpr int kCols = 32;  // query rows of an item (columns of the tiles)
+
+// ---------------------------------------------------------------------------
+// plan (host)
+// ---------------------------------------------------------------------------
+struct LatPlan {
+  int nu;      // units (32 columns) of a cache row
+  int vu;      // units that hold latents
+  int ncw;     // column waves: each holds nuw units of the row
+  int ntw;     // token waves: each takes 32 tokens of a step
+  int nuw;     // units a wave holds
+  int upw;     // ... and the kernel's register class for them
+  int stages;  // tiles in LDS per wave
+  int tpt;     // tokens of a tile (32, or 16 where 32 do not fit)
+  int step;    // tokens of a step: tpt ntw
+  int rps;     // 16-byte pieces of an LDS row (an odd number of units)
+  int tile_bytes, xchg_bytes;
+  size_t lds;
+  int G;       // workgroups of split
+};
+
+__host__ LatPlan lat_plan(int r, int d_rope, int es) {
+  LatPlan p{};
+  p.nu = latent_row(r, d_rope) / kRowUnit;
+  p.vu = (2 * r + 31) / 32;
+  // a wave's registers hold 12 units (q' and the sums); wider rows go to four waves
+  p.ncw = p.nu <= 12 ? 1 : 4;
+  p.nuw = (p.nu + p.ncw - 1) / p.ncw;
+  p.upw = p.nuw <= 4 ? 4 : p.nuw <= 8 ? 8 : 12;
+  const int pu = es * 2;
+  p.rps = pu * (p.nuw | 1);
+  p.tpt = 32;
+  p.tile_bytes = 32 * 16 * p.rps;
+  if (p.ncw == 1) {
+    // as many token waves as two tiles each leave room for
+    p.ntw = 8 * static_cast<size_t>(p.tile_bytes) <= kLdsMax ? 4 : 2;
+    p.stages = 2 * static_cast<size_t>(p.ntw) * p.tile_bytes <= kLdsMax ? 2 : 1;
+  } else {
+    p.ntw = 1;
+    p.xchg_bytes = 2 * p.ncw * 4096;  // partial scores, two buffers
+    if (static_cast<size_t>(p.ncw) * p.tile_bytes + p.xchg_bytes > kLdsMax) p.tpt = 16, p.tile_bytes /= 2;
+    p.stages = 2 * static_cast<size_t>(p.ncw) * p.tile_bytes + p.xchg_bytes <= kLdsMax ? 2 : 1;
+  }
+  p.step = p.tpt * p.ntw;
+  const int nw = p.ncw * p.ntw;
+  p.lds = static_cast<size_t>(nw) * p.stages * p.tile_bytes + p.xchg_bytes;
+  if (p.ncw == 1) {
+    // the token waves' sums are added through the same memory
+    const size_t red = static_cast<size_t>(p.ntw) * kCols * (p.vu * 32 + 4) * 4 + p.ntw * kCols * 8;
+    if (red > p.lds) p.lds = red;
+  }
+  p.G = 256;
+  return p;
+}
+
+// terms of q' and of the probabilities by the cache's type and the activations'
+constexpr int terms_q(int cd, bool f32) { return cd == kDtF32 ? 1 : (cd == kDtBF16 && f32 ? 3 : 2); }
+constexpr int terms_p(int cd, bool f32) { return cd == kDtF32 || !f32 ? 1 : (cd == kDtBF16 ? 3 : 2); }
+
+struct LatWs {
+  size_t q_off, qs_off, ml_off, o_off, bytes;
+};
+// Sized for every type pair: three terms of 2 bytes cover two of 2 and one of 4.
+__host__ LatWs lat_ws(int64_t T, int64_t n_seq, int64_t H, int r, int d_rope) {
+  LatWs w{};
+  const int64_t row = latent_row(r, d_rope), ow = (2 * r + 31) / 32 * 32;
+  const int64_t slots = 256 + (T * H + kCols - 1) / kCols + n_seq;
+  auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+  w.qs_off = up(static_cast<size_t>(T * H * row) * 6);
+  w.ml_off = w.qs_off + up(static_cast<size_t>(T * H) * 4);
+  w.o_off = w.ml_off + up(static_cast<size_t>(slots) * kCols * 8);
+  w.bytes = w.o_off + up(static_cast<size_t>(slots) * kCols * ow * 4);
+  return w;
+}
+
+// ---------------------------------------------------------------------------
+// work map: sequence b has ceil(nq_b H / 32) items of ceil(len_b / step) steps each;
+// all W steps in a row are dealt to G workgroups (at most W), g taking [W g / G, W (g + 1) / G);
+// its part of the item numbered i over all sequences goes to slot g + i, so that an
+// item's slots are consecutive and no two meet
+// ---------------------------------------------------------------------------
+struct SeqWork {
+  int q0, nq;       // first token, tokens
+  int len;          // cached tokens, within the page table
+  int items, steps;  // items, steps of each
+};
+__device__ __forceinline__ SeqWork seq_work(const CacheArgs& c, int b, int T, int H, int step) {
+  SeqWork s;
+  int hi;
+  seq_range(c.cu, b, T, s.q0, hi);
+  s.nq = hi - s.q0;
+  s.len = static_cast<int>(
+      max(int64_t(0), min(static_cast<int64_t>(c.lens[b]), static_cast<int64_t>(c.max_pages) * c.page_size)));
+  s.items = static_cast<int>((static_cast<int64_t>(s.nq) * H + kCols - 1) / kCols);
+  s.steps = (s.len + step - 1) / step;
+  return s;
+}
+__device__ __forceinline__ int64_t wave_scan(int64_t v, int lane) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int64_t o = __shfl_up(v, s);
+    if (lane >= s) v += o;
+  }
+  return v;
+}
+// all steps of all sequences (every lane)
+__device__ __forceinline__ int64_t total_work(const CacheArgs& c, int T, int H, int step, int lane) {
+  int64_t w = 0;
+  for (int b = lane; b < c.n_seq; b += 64) {
+    const SeqWork s = seq_work(c, b, T, H, step);
+    w += static_cast<int64_t>(s.items) * s.steps;
+  }
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) w += __shfl_xor(w, s);
+  return w;
+}
+// The sequence that `find` picks by (b, first step, first item, its work): the first one
+// with by_step ? start + work > x : b == x.  Returns b (-1: none) and the sums before it.
+__device__ __forceinline__ int find_work(const CacheArgs& c, int T, int H, int step, int lane, bool by_step, int64_t x,
+                                         int64_t& steps_before, int64_t& items_before) {
+  int64_t sb = 0, ib = 0;
+  for (int b0 = 0; b0 < c.n_seq; b0 += 64) {
+    const int b = b0 + lane;
+    int64_t w = 0, it = 0;
+    if (b < c.n_seq) {
+      const SeqWork s = seq_work(c, b, T, H, step);
+      w = static_cast<int64_t>(s.items) * s.steps, it = s.items;
+    }
+    const int64_t ws = wave_scan(w, lane), is = wave_scan(it, lane);
+    const uint64_t m = __ballot(b < c.n_seq && (by_step ? sb + ws > x : b == x));
+    if (m != 0) {
+      const int k = __builtin_ctzll(m);
+      steps_before = sb + __shfl(ws, k) - __shfl(w, k);
+      items_before = ib + __shfl(is, k) - __shfl(it, k);
+      return b0 + k;
+    }
+    sb += __shfl(ws, 63);
+    ib += __shfl(is, 63);
+  }
+  return -1;
+}
+
+// the sequence of token t (-1: none)
+__device__ __forceinline__ int seq_of(const CacheArgs& c, int t, int T, int lane) {
+  for (int b0 = 0; b0 < c.n_seq; b0 += 64) {
+    int lo = 0, hi = 0;
+    if (b0 + lane < c.n_seq) seq_range(c.cu, b0 + lane, T, lo, hi);
+    const uint64_t m = __ballot(lo <= t && t < hi);
+    if (m != 0) return b0 + __builtin_ctzll(m);
+  }
+  return -1;
+}
+
+// x[8] as N terms of type CD, each the rounding of what the previous ones left
+template <int CD, int N>
+__device__ __forceinline__ void to_terms(float (&x)[8], Frag<CD> (&f)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    f[n] = frag_from<CD>(x);
+    if (n + 1 < N) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] -= frag_elem<CD>(f[n], e);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// absorb
+// ---------------------------------------------------------------------------
+constexpr int kAThreads = 256;
+constexpr int kMaxHead = 256;  // widths of a head
+
+// A workgroup per (token, head): the words of the head's rows of U (both paths) and
+// h (.) q in LDS, a thread per latent adds its column with the signs of its bit.
+template <int DT, int SC, int CD, int TQ>
+__global__ void __launch_bounds__(kAThreads) absorb_kernel(LatentAttnArgs a, char* qout, float* qsc) {
+  __shared__ float hq[2][kMaxHead];
+  __shared__ float qv[kMaxLatentRow];
+  __shared__ float red[kAThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H;
+  const CacheArgs& c = a.c;
+  const int r = c.r, dn = a.d_nope, dr = c.d_rope, row = c.row;
+  const int n_out = a.Hk * (dn + a.d_v), i0 = h / (a.H / a.Hk) * dn;
+  const char* q = static_cast<const char*>(a.q) + (t * a.q_t + h * a.q_h) * esize<DT>();
+  for (int i = tid; i < 2 * dn; i += kAThreads) {
+    const int p = i >= dn, j = i - p * dn;
+    hq[p][j] = ld<SC>(a.h[p], i0 + j) * ld<DT>(q, j);
+  }
+  int pos = 0;
+  if (dr > 0) {
+    const int b = seq_of(c, t, a.T, lane);
+    if (b >= 0) {
+      const SeqWork s = seq_work(c, b, a.T, a.H, 32);
+      pos = max(0, s.len - s.nq + (t - s.q0));
+    }
+  }
+  __syncthreads();
+  float top = 0.0f;
+  for (int k = tid; k < row; k += kAThreads) {
+    float v = 0.0f;
+    if (k < 2 * r) {
+      const int p = k >= r, kk = k - p * r;
+      const PackedView u{static_cast<const uint32_t*>(a.U[p]), n_out, r >> 5, r & 31};
+      const int kb = kk >> 5, sh = 31 - (kk & 31);
+      float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+      int i = 0;
+      for (; i + 4 <= dn; i += 4) {
+        const uint32_t w0 = load_word(u, kb, i0 + i), w1 = load_word(u, kb, i0 + i + 1);
+        const uint32_t w2 = load_word(u, kb, i0 + i + 2), w3 = load_word(u, kb, i0 + i + 3);
+        s0 += __uint_as_float(__float_as_uint(hq[p][i]) ^ ((w0 << sh) & 0x80000000u));
+        s1 += __uint_as_float(__float_as_uint(hq[p][i + 1]) ^ ((w1 << sh) & 0x80000000u));
+        s2 += __uint_as_float(__float_as_uint(hq[p][i + 2]) ^ ((w2 << sh) & 0x80000000u));
+        s3 += __uint_as_float(__float_as_uint(hq[p][i + 3]) ^ ((w3 << sh) & 0x80000000u));
+      }
+      for (; i < dn; ++i)
+        s0 += __uint_as_float(__float_as_uint(hq[p][i]) ^ ((load_word(u, kb, i0 + i) << sh) & 0x80000000u));
+      v = (s0 + s1) + (s2 + s3);
+    } else if (k < 2 * r + dr) {
+      const int i = k - 2 * r, half = dr / 2;
+      v = ld<DT>(q, dn + i);
+      if (a.freqs != nullptr) {
+        const bool low = i < half;
+        float cs, sn;
+        turn_of(pos, a.freqs[low ? i : i - half], cs, sn);
+        const float o = ld<DT>(q, dn + (low ? i + half : i - half));
+        v = low ? v * cs - o * sn : v * cs + o * sn;
+      }
+    }
+    qv[k] = v;
+    top = fmaxf(top, fabsf(v));
+  }
+  float f = 1.0f;
+  if constexpr (CD == kDtF16) {
+    // q' may leave f16's range: rows are brought to a maximum in [1/2, 1) by a power of two
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    if (lane == 0) red[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    if (top > 0.0f && top < 1e38f) {
+      int ex;
+      frexpf(top, &ex);
+      f = ldexpf(1.0f, max(-120, min(120, -ex)));
+    }
+  }
+  __syncthreads();
+  const int64_t m = static_cast<int64_t>(t) * a.H + h;
+  if (tid == 0) qsc[m] = a.scale * kLog2e / f;
+  char* out = qout + m * TQ * row * esize<CD>();
+  for (int k = 8 * tid; k < row; k += 8 * kAThreads) {
+    float x[8];
+    Frag<CD> fr[TQ];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = qv[k + e] * f;
+    to_terms<CD, TQ>(x, fr);
+#pragma unroll
+    for (int n = 0; n < TQ; ++n) {
+      char* p = out + (n * row + k) * esize<CD>();
+      *reinterpret_cast<u32x4*>(p) = fr[n].v[0];
+      if constexpr (CD == kDtF32) *reinterpret_cast<u32x4*>(p + 16) = fr[n].v[1];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// split
+// ---------------------------------------------------------------------------
+struct SplitArgs {
+  CacheArgs c;
+  LatPlan p;
+  int T, H;
+  uint32_t magic;  // lin / rps
+  const char* q;
+  const float* qsc;
+  float* ml;
+  float* o;
+};
+
+// An LDS tile holds 32 tokens' columns of one wave, rows of rps pieces (16 bytes);
+// piece q of row t stands at q with its place in the unit exchanged by swz(t), which
+// with an odd number of units a row makes the row-wise reads free of bank conflicts
+// and the transposed ones even.
+template <int CD>
+__device__ __forceinline__ int swz(int t) {
+  return CD == kDtF32 ? (t >> 1) & 7 : (t >> 2) & 3;
+}
+template <int CD>
+__device__ __forceinline__ Frag<CD> tile_rows(const char* t, int rps, int chunk, int lane, int tpt) {
+  constexpr int PU = 2 * esize<CD>();
+  const int row = lane & (tpt - 1), s = swz<CD>(row);
+  const char* p = t + row * rps * 16;
+  Frag<CD> f;
+  if constexpr (CD == kDtF32) {
+    const int q = 4 * chunk + 2 * (lane >> 5);  // two pieces
+    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * ((q & ~(PU - 1)) | ((q ^ s) & (PU - 1))));
+    f.v[1] = *reinterpret_cast<const u32x4*>(p + 16 * ((q & ~(PU - 1)) | (((q + 1) ^ s) & (PU - 1))));
+  } else {
+    const int q = 2 * chunk + (lane >> 5);
+    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * ((q & ~(PU - 1)) | ((q ^ s) & (PU - 1))));
+  }
+  return f;
+}
+// columns 32 u + lane % 32 at the 16 tokens of slice s (slots as in attn_common.h)
+template <int CD>
+__device__ __forceinline__ Frag<CD> tile_cols(const char* t, int rps, int s, int u, int lane) {
+  Frag<CD> f;
+  const int hh = lane >> 5;
+  if constexpr (CD == kDtF32) {
+    const int q = (lane & 31) >> 2;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int row = 16 * s + 8 * (k >> 2) + 4 * hh + (k & 3);
+      f.v[k >> 2][k & 3] = *reinterpret_cast<const uint32_t*>(t + row * rps * 16 + 16 * (8 * u + (q ^ swz<CD>(row))) +
+                                                              4 * (lane & 3));
+    }
+  } else {
+    typedef __attribute__((address_space(3))) s16x4* lds4;
+    const int i = lane & 15, q = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+    const int row = 16 * s + 4 * hh + (i >> 2);
+    const char* p0 = t + row * rps * 16 + 16 * (4 * u + (q ^ swz<CD>(row))) + 8 * (i & 1);
+    const char* p1 = t + (row + 8) * rps * 16 + 16 * (4 * u + (q ^ swz<CD>(row + 8))) + 8 * (i & 1);
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0)));
+    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1)));
+    f.v[0] = u32x4{a[0], a[1], b[0], b[1]};
+  }
+  return f;
+}
+
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xf70);  // vmcnt(0); LDS and scalar counters left alone
+  asm volatile("" ::: "memory");
+}
+
+template <int CD, int TQ, int TP, int UPW, bool CSPLIT>
+__global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  constexpr int PU = 2 * esize<CD>();
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hh = lane >> 5, ml_ = lane & 31;
+  const CacheArgs& c = a.c;
+  const LatPlan& p = a.p;
+  const int step = p.step;
+  const int64_t W = total_work(c, a.T, a.H, step, lane);
+  const int g = blockIdx.x;
+  const int64_t G = min(static_cast<int64_t>(p.G), W);  // no workgroup with a share is without a step
+  if (g >= G) return;
+  int64_t x = W * g / G;
+  const int64_t x_end = W * (g + 1) / G;
+  const int tw = CSPLIT ? 0 : wave, cw = CSPLIT ? wave : 0;
+  const int u0 = cw * p.nuw;                                       // the wave's units of the row
+  const int nu = max(0, min(p.nuw, p.nu - u0)), vu = max(0, min(nu, p.vu - u0));
+  char* tiles = smem + wave * p.stages * p.tile_bytes;
+  float* xchg = reinterpret_cast<float*>(smem + (CSPLIT ? 4 : p.ntw) * p.stages * p.tile_bytes);
+  const int n_ld = p.rps * p.tpt / 64;
+  const int64_t row_bytes = static_cast<int64_t>(c.row) * esize<CD>();
+  const char* data = static_cast<const char*>(c.data) + u0 * 32 * esize<CD>();
+  const int ow = p.vu * 32;
+
+  while (x < x_end) {
+    int64_t sb, ib;
+    const int b = find_work(c, a.T, a.H, step, lane, true, x, sb, ib);
+    if (b < 0) break;
+    const SeqWork sw = seq_work(c, b, a.T, a.H, step);
+    const int item = static_cast<int>((x - sb) / sw.steps);
+    const int s0 = static_cast<int>((x - sb) - static_cast<int64_t>(item) * sw.steps);
+    const int s1 = static_cast<int>(min(static_cast<int64_t>(sw.steps), s0 + (x_end - x)));
+    const int64_t slot = g + ib + item;
+    x += s1 - s0;
+
+    // the item's query rows: columns of the tiles
+    const int rows = sw.nq * a.H;
+    const int rr = min(item * kCols + ml_, rows - 1);
+    const int64_t m_row = static_cast<int64_t>(sw.q0) * a.H + rr;
+    const int first = sw.len - sw.nq;  // position of the sequence's first query
+    const int pos = first + rr / a.H;
+    const int pos_min = first + item * kCols / a.H;
+    const float qs = a.qsc[m_row];
+    Frag<CD> qf[2 * UPW][TQ];
+#pragma unroll
+    for (int k = 0; k < 2 * UPW; ++k) {
+#pragma unroll
+      for (int n = 0; n < TQ; ++n) {
+        qf[k][n] = frag_zero<CD>();
+        if (k < 2 * nu) {
+          const char* src = a.q + ((m_row * TQ + n) * c.row + 32 * u0 + 16 * k + 8 * hh) * esize<CD>();
+          qf[k][n].v[0] = *reinterpret_cast<const u32x4*>(src);
+          if constexpr (CD == kDtF32) qf[k][n].v[1] = *reinterpret_cast<const u32x4*>(src + 16);
+        }
+      }
+    }
+    // a token's page; its row of the cache, where the page is one.  Token 0 stands in for
+    // tokens without a place: every row sees it, so that what the masked scores' zero
+    // probabilities are multiplied with is no stranger's infinity.
+    auto page_of = [&](int tok) {
+      return c.table[static_cast<int64_t>(b) * c.max_pages + min(tok, sw.len - 1) / c.page_size];
+    };
+    auto place = [&](int tok, int page, bool& ok) {
+      ok = tok < sw.len && page >= 0 && page < c.n_pages;
+      return page * c.page_size + tok % c.page_size;
+    };
+    bool ok0;
+    const int at0 = place(0, page_of(0), ok0);
+    const int place0 = ok0 ? at0 : 0;
+    auto issue = [&](int tok, int page, char* dst) -> uint32_t {
+      bool ok;
+      const int at = place(tok, page, ok);
+      const int idx = ok ? at : place0;
+      ok = ok && ml_ < p.tpt;
+      for (int i = 0; i < n_ld; ++i) {
+        const uint32_t lin = 64 * i + lane;
+        const int t = __umulhi(lin, a.magic), q = lin - t * p.rps;
+        const int piece = q < PU * nu ? (q & ~(PU - 1)) | ((q ^ swz<CD>(t)) & (PU - 1)) : 0;
+        const char* src = data + __shfl(idx, t) * row_bytes + 16 * piece;
+        __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(dst + 1024 * i), 16, 0, 0);
+      }
+      return static_cast<uint32_t>(__ballot(ok));  // lanes 0 .. 31: the tile's tokens
+    };
+
+    floatx16 o[UPW];
+#pragma unroll
+    for (int u = 0; u < UPW; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[u][e] = 0.0f;
+    float mx = -INFINITY, sum = 0.0f;
+    auto tile_at = [&](int s) { return (s * p.ntw + tw) * p.tpt; };
+    uint32_t okm = 0, okn = 0;
+    int page = page_of(tile_at(s0) + ml_);
+    __syncthreads();  // the previous item's readers of this memory are done
+    if (p.stages == 2) {
+      okm = issue(tile_at(s0) + ml_, page, tiles);
+      page = page_of(tile_at(s0 + 1) + ml_);
+    }
+    for (int s = s0; s < s1; ++s) {
+      char* tile = tiles;
+      if (p.stages == 2) {
+        tile += ((s - s0) & 1) * p.tile_bytes;
+        wait_loads();
+        if (s + 1 < s1) {
+          okn = issue(tile_at(s + 1) + ml_, page, tiles + ((s + 1 - s0) & 1) * p.tile_bytes);
+          page = page_of(tile_at(s + 2) + ml_);
+        }
+      } else {
+        okm = issue(tile_at(s) + ml_, page, tile);
+        page = page_of(tile_at(s + 1) + ml_);
+        wait_loads();
+      }
+      asm volatile("" ::: "memory");
+      // scores: row (token) 8 (e / 4) + 4 hh + e % 4 of column (query row) lane % 32
+      floatx16 acc;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 2 * UPW; ++k) {
+        if (k < 2 * nu) {
+          const Frag<CD> kf = tile_rows<CD>(tile, p.rps, k, lane, p.tpt);
+#pragma unroll
+          for (int n = 0; n < TQ; ++n) acc = mma32<CD>(kf, qf[k][n], acc);
+        }
+      }
+      if constexpr (CSPLIT) {
+        // the column waves' scores added, in the same order by each of them
+        float* xb = xchg + ((s - s0) & 1) * 4096;
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<float4*>(xb + wave * 1024 + (e >> 2) * 256 + lane * 4) =
+              make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          float4 t = *reinterpret_cast<const float4*>(xb + (e >> 2) * 256 + lane * 4);
+#pragma unroll
+          for (int w = 1; w < 4; ++w) {
+            const float4 v = *reinterpret_cast<const float4*>(xb + w * 1024 + (e >> 2) * 256 + lane * 4);
+            t.x += v.x, t.y += v.y, t.z += v.z, t.w += v.w;
+          }
+          acc[e] = t.x, acc[e + 1] = t.y, acc[e + 2] = t.z, acc[e + 3] = t.w;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[e] *= qs;
+      const int base = tile_at(s);
+      if (okm != 0xffffffffu || base + 31 > pos_min) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int t = 8 * (e >> 2) + 4 * hh + (e & 3);
+          if (!((okm >> t) & 1u) || base + t > pos) acc[e] = -INFINITY;
+        }
+      }
+      float tm = acc[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) tm = fmaxf(tm, acc[e]);
+      tm = fmaxf(tm, __shfl_xor(tm, 32));
+      if (__any(tm > mx)) {
+        const float m2 = fmaxf(mx, tm);
+        const float f = m2 == -INFINITY ? 1.0f : exp2f(mx - m2);
+        mx = m2;
+        sum *= f;
+#pragma unroll
+        for (int u = 0; u < UPW; ++u) {
+          if (u < vu) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[u][e] *= f;
+          }
+        }
+      }
+      const float mz = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        acc[e] = exp2f(acc[e] - mz);
+        sum += acc[e];
+      }
+#pragma unroll
+      for (int sl = 0; sl < 2; ++sl) {
+        if (16 * sl >= p.tpt) break;
+        // probabilities in the cache's type: with 16-bit activations one rounding (relative
+        // half a step each, of terms that the output averages), with fp32 ones TP terms
+        float pv[8];
+        Frag<CD> pf[TP];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pv[e] = acc[8 * sl + e];
+        to_terms<CD, TP>(pv, pf);
+#pragma unroll
+        for (int u = 0; u < UPW; ++u) {
+          if (u < vu) {
+            const Frag<CD> vf = tile_cols<CD>(tile, p.rps, sl, u, lane);
+#pragma unroll
+            for (int n = 0; n < TP; ++n) o[u] = mma32<CD>(vf, pf[n], o[u]);
+          }
+        }
+      }
+      if (p.stages == 2) okm = okn;
+      asm volatile("" ::: "memory");
+    }
+
+    // the item's partial result: sums of each column scaled by its maximum's exponential
+    sum += __shfl_xor(sum, 32);
+    float* po = a.o + slot * kCols * ow;
+    float* pm = a.ml + slot * kCols * 2;
+    if constexpr (CSPLIT) {
+#pragma unroll
+      for (int u = 0; u < UPW; ++u) {
+        if (u < vu) {
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<float4*>(po + ml_ * ow + 32 * (u0 + u) + 2 * e + 4 * hh) =
+                make_float4(o[u][e], o[u][e + 1], o[u][e + 2], o[u][e + 3]);
+        }
+      }
+      if (wave == 0 && hh == 0) pm[2 * ml_] = mx, pm[2 * ml_ + 1] = sum;
+    } else {
+      __syncthreads();  // every wave is done with its tiles
+      const int st = ow + 4;
+      float* red = reinterpret_cast<float*>(smem);
+      float* rml = red + p.ntw * kCols * st;
+#pragma unroll
+      for (int u = 0; u < UPW; ++u) {
+        if (u < vu) {
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<float4*>(red + (wave * kCols + ml_) * st + 32 * u + 2 * e + 4 * hh) =
+                make_float4(o[u][e], o[u][e + 1], o[u][e + 2], o[u][e + 3]);
+        }
+      }
+      if (hh == 0) rml[(wave * kCols + ml_) * 2] = mx, rml[(wave * kCols + ml_) * 2 + 1] = sum;
+      __syncthreads();
+      const int nq4 = ow / 4;
+      for (int i = tid; i < kCols * nq4; i += 64 * p.ntw) {
+        const int m = i / nq4, cq = i - m * nq4;
+        float top = -INFINITY;
+        for (int w = 0; w < p.ntw; ++w) top = fmaxf(top, rml[(w * kCols + m) * 2]);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float l = 0.0f;
+        for (int w = 0; w < p.ntw; ++w) {
+          const float f = top == -INFINITY ? 0.0f : exp2f(rml[(w * kCols + m) * 2] - top);
+          const float4 t = *reinterpret_cast<const float4*>(red + (w * kCols + m) * st + 4 * cq);
+          v.x += f * t.x, v.y += f * t.y, v.z += f * t.z, v.w += f * t.w;
+          l += f * rml[(w * kCols + m) * 2 + 1];
+        }
+        *reinterpret_cast<float4*>(po + m * ow + 4 * cq) = v;
+        if (cq == 0) pm[2 * m] = top, pm[2 * m + 1] = l;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// join
+// ---------------------------------------------------------------------------
+constexpr int kJThreads = 256;
+
+struct JoinArgs {
+  LatentAttnArgs a;
+  LatPlan p;
+  const float* ml;
+  const float* o;
+};
+
+// A workgroup per (token, head): the partial sums of its row, in workgroup order,
+// then its head's rows of U with h.
+template <int DT, int SC>
+__global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
+  __shared__ float wt[256];
+  __shared__ __attribute__((aligned(16))) float ov[2][kMaxLatentRank];
+  __shared__ float part[2][kMaxHead];
+  const LatentAttnArgs& a = j.a;
+  const CacheArgs& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H;
+  const int b = seq_of(c, t, a.T, lane);
+  if (b < 0) return;  // a row behind the last sequence
+  const int step = j.p.step, r = c.r, rp = (r + 31) & ~31;
+  const SeqWork sw = seq_work(c, b, a.T, a.H, step);
+  char* out = static_cast<char*>(a.out) + (static_cast<int64_t>(t) * a.H + h) * a.d_v * esize<DT>();
+  if (sw.steps == 0) {
+    for (int i = tid; i < a.d_v; i += kJThreads) st<DT>(out, i, 0.0f);
+    return;
+  }
+  const int64_t W = total_work(c, a.T, a.H, step, lane);
+  int64_t sb = 0, ib = 0;
+  find_work(c, a.T, a.H, step, lane, false, b, sb, ib);
+  const int rr = (t - sw.q0) * a.H + h, item = rr / kCols, m = rr - item * kCols;
+  const int64_t x0 = sb + static_cast<int64_t>(item) * sw.steps;
+  const int64_t G = min(static_cast<int64_t>(j.p.G), W);
+  const int g0 = static_cast<int>(((x0 + 1) * G - 1) / W), g1 = static_cast<int>(((x0 + sw.steps) * G - 1) / W);
+  const int n = g1 - g0 + 1;  // <= G
+  const int64_t slot0 = g0 + ib + item;
+  const int ow = j.p.vu * 32;
+  float top = -INFINITY;
+  for (int i = lane; i < n; i += 64) top = fmaxf(top, j.ml[((slot0 + i) * kCols + m) * 2]);
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+  float l = 0.0f;
+  for (int i = lane; i < n; i += 64) {
+    const float* q = j.ml + ((slot0 + i) * kCols + m) * 2;
+    const float f = top == -INFINITY ? 0.0f : exp2f(q[0] - top);
+    l += f * q[1];
+    if (tid < 64) wt[i] = f;
+  }
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) l += __shfl_xor(l, s);
+  const float inv = top == -INFINITY ? 0.0f : 1.0f / l;
+  for (int i = tid; i < 2 * (rp - r); i += kJThreads) {
+    const int p = i >= rp - r;
+    ov[p][r + i - p * (rp - r)] = 0.0f;
+  }
+  __syncthreads();
+  const float* po = j.o + (slot0 * kCols + m) * ow;
+  for (int k = tid; k < 2 * r; k += kJThreads) {
+    float v = 0.0f;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) v += wt[i] * po[static_cast<int64_t>(i) * kCols * ow + k];
+    ov[k >= r][k >= r ? k - r : k] = v * inv;
+  }
+  __syncthreads();
+  const int n_out = a.Hk * (a.d_nope + a.d_v), row0 = a.Hk * a.d_nope + h / (a.H / a.Hk) * a.d_v;
+  for (int q = tid; q < 2 * a.d_v; q += kJThreads) {
+    const int p = q >= a.d_v, i = q - p * a.d_v;
+    const PackedView u{static_cast<const uint32_t*>(a.U[p]), n_out, r >> 5, r & 31};
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int kb = 0; kb < rp / 32; ++kb) {
+      const uint32_t w = load_word(u, kb, row0 + i);
+#pragma unroll
+      for (int k = 0; k < 32; k += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(&ov[p][32 * kb + k]);
+        const float vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s[e] += __uint_as_float(__float_as_uint(vv[e]) ^ ((w << (31 - k - e)) & 0x80000000u));
+      }
+    }
+    part[p][i] = ld<SC>(a.h[p], row0 + i) * ((s[0] + s[1]) + (s[2] + s[3]));
+  }
+  __syncthreads();
+  for (int i = tid; i < a.d_v; i += kJThreads) st<DT>(out, i, part[0][i] + part[1][i]);
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+template <int CD, int TQ, int TP, int UPW, bool CS>
+hipError_t split_launch(const SplitArgs& s, hipStream_t stream) {
+  static LdsLimit limit;
+  const hipError_t e = raise_lds(reinterpret_cast<const void*>(&split_kernel<CD, TQ, TP, UPW, CS>), s.p.lds, limit);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((split_kernel<CD, TQ, TP, UPW, CS>), dim3(s.p.G), dim3(64 * s.p.ncw * s.p.ntw), s.p.lds, stream, s);
+  return hipGetLastError();
+}
+template <int CD, int TQ, int TP>
+hipError_t split_cd(const SplitArgs& s, hipStream_t stream) {
+  if (s.p.ncw == 1) {
+    switch (s.p.upw) {
+      case 4: return split_launch<CD, TQ, TP, 4, false>(s, stream);
+      case 8: return split_launch<CD, TQ, TP, 8, false>(s, stream);
+      default: return split_launch<CD, TQ, TP, 12, false>(s, stream);
+    }
+  }
+  switch (s.p.upw) {
+    case 4: return split_launch<CD, TQ, TP, 4, true>(s, stream);
+    case 8: return split_launch<CD, TQ, TP, 8, true>(s, stream);
+    default: return split_launch<CD, TQ, TP, 12, true>(s, stream);
+  }
+}
+
+template <int DT, int SC, int CD>
+hipError_t run(const LatentAttnArgs& a, hipStream_t stream) {
+  constexpr int TQ = terms_q(CD, DT == kDtF32), TP = terms_p(CD, DT == kDtF32);
+  const LatPlan p = lat_plan(a.c.r, a.c.d_rope, esize<CD>());
+  const LatWs w = lat_ws(a.T, a.c.n_seq, a.H, a.c.r, a.c.d_rope);
+  char* ws = static_cast<char*>(a.ws);
+  float* qsc = reinterpret_cast<float*>(ws + w.qs_off);
+  hipLaunchKernelGGL((absorb_kernel<DT, SC, CD, TQ>), dim3(a.T * a.H), dim3(kAThreads), 0, stream, a, ws, qsc);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  SplitArgs s{};
+  s.c = a.c;
+  s.p = p;
+  s.T = a.T, s.H = a.H;
+  s.magic = static_cast<uint32_t>(((uint64_t(1) << 32) + p.rps - 1) / p.rps);
+  s.q = ws, s.qsc = qsc;
+  s.ml = reinterpret_cast<float*>(ws + w.ml_off);
+  s.o = reinterpret_cast<float*>(ws + w.o_off);
+  e = split_cd<CD, TQ, TP>(s, stream);
+  if (e != hipSuccess) return e;
+  JoinArgs j{a, p, s.ml, s.o};
+  hipLaunchKernelGGL((join_kernel<DT, SC>), dim3(a.T * a.H), dim3(kJThreads), 0, stream, j);
+  return hipGetLastError();
+}
+template <int DT, int SC>
+hipError_t run_sc(const LatentAttnArgs& a, hipStream_t stream) {
+  switch (a.c.dt) {
+    case kDtF32: return run<DT, SC, kDtF32>(a, stream);
+    case kDtF16: return run<DT, SC, kDtF16>(a, stream);
+    default: return run<DT, SC, kDtBF16>(a, stream);
+  }
+}
+template <int DT>
+hipError_t run_dt(const LatentAttnArgs& a, hipStream_t stream) {
+  switch (a.sc_dt) {
+    case kDtF32: return run_sc<DT, kDtF32>(a, stream);
+    case kDtF16: return run_sc<DT, kDtF16>(a, stream);
+    default: return run_sc<DT, kDtBF16>(a, stream);
+  }
+}
+
+}  // namespace
+
+size_t latent_attn_workspace_bytes(int T, int n_seq, int H, int r, int d_rope) {
+  return lat_ws(T, n_seq, H, r, d_rope).bytes;
+}
+
+hipError_t launch_latent_attn(const LatentAttnArgs& a, hipStream_t stream) {
+  switch (a.dt) {
+    case kDtF32: return run_dt<kDtF32>(a, stream);
+    case kDtF16: return run_dt<kDtF16>(a, stream);
+    default: return run_dt<kDtBF16>(a, stream);
+  }
+}
+
+}  // namespace lb
