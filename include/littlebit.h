@@ -526,8 +526,8 @@ lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const vo
    multiple of Hk; d_nope, d_v <= 256 (LB_ERR_SHAPE); scale finite and > 0
    (LB_ERR_ARG).  q' enters the scores with at least 16 significant bits (24 for
    fp32 activations), softmax statistics and sums are fp32; probabilities enter
-   the sums with 8 bits (a bf16 cache), 11 (f16), 24 (an fp32 cache, or fp32
-   activations; 22 of them on an f16 cache).
+   the sums rounded to the cache's type where out's is no finer, else in two or
+   three terms of it (22 bits or more for fp32 activations).
    workspace: 256-byte aligned, >= lb_latent_attention_workspace_bytes(T, n_seq,
    H, r, d_rope) bytes (0 for invalid sizes), no zero-fill needed; calls that may
    run concurrently need distinct workspaces.  Repeated calls give the same bits. */

@@ -55,7 +55,7 @@ __host__ LatPlan lat_plan(int r, int d_rope, int es) {
   // a wave's registers hold 12 units (q' and the sums); wider rows go to four waves
   p.ncw = p.nu <= 12 ? 1 : 4;
   p.nuw = (p.nu + p.ncw - 1) / p.ncw;
-  p.upw = p.nuw <= 4 ? 4 : p.nuw <= 8 ? 8 : 12;
+  p.upw = p.nuw <= 4 ? 4 : (p.nuw + 1) / 2 * 2;
   const int pu = es * 2;
   p.rps = pu * (p.nuw | 1);
   p.tpt = 32;
@@ -84,7 +84,9 @@ __host__ LatPlan lat_plan(int r, int d_rope, int es) {
 
 // terms of q' and of the probabilities by the cache's type and the activations'
 constexpr int terms_q(int cd, bool f32) { return cd == kDtF32 ? 1 : (cd == kDtBF16 && f32 ? 3 : 2); }
-constexpr int terms_p(int cd, bool f32) { return cd == kDtF32 || !f32 ? 1 : (cd == kDtBF16 ? 3 : 2); }
+constexpr int terms_p(int cd, int act) {
+  return cd == kDtF32 || act == kDtBF16 || (act == kDtF16 && cd == kDtF16) ? 1 : (cd == kDtBF16 && act == kDtF32 ? 3 : 2);
+}
 
 struct LatWs {
   size_t q_off, qs_off, ml_off, o_off, bytes;
@@ -193,101 +195,159 @@ __device__ __forceinline__ void to_terms(float (&x)[8], Frag<CD> (&f)[N]) {
   }
 }
 
+// x rounded to type CD, as fp32
+template <int CD>
+__device__ __forceinline__ float rounded(float x) {
+  if constexpr (CD == kDtF32) return x;
+  if constexpr (CD == kDtBF16) return bf16_bits_to_f32(f32_to_bf16_bits(x));
+  asm volatile("" : "+v"(x));
+  return __half2float(__float2half_rn(x));
+}
+
 // ---------------------------------------------------------------------------
 // absorb
 // ---------------------------------------------------------------------------
-constexpr int kAThreads = 256;
-constexpr int kMaxHead = 256;  // widths of a head
+constexpr int kMaxHead = 256;    // widths of a head
+constexpr int kRopeHeads = 8;    // heads of a rotary workgroup
+constexpr int kAbsTokens = 32;   // tokens of a tile
 
-// A workgroup per (token, head): the words of the head's rows of U (both paths) and
-// h (.) q in LDS, a thread per latent adds its column with the signs of its bit.
+// With an f16 cache q' is brought into f16's range by a power of two per row: the
+// inverse of a bound on the row's values (order-free maxima, so that every workgroup
+// finds the same one).  top: the largest |h (.) q|, rope: of the rotary part.
+__device__ __forceinline__ float row_factor(float top, float rope, int dn) {
+  const float b = fmaxf(top * static_cast<float>(dn), 1.5f * rope);
+  if (!(b > 0.0f) || b > 1e38f) return 1.0f;
+  int ex;
+  frexpf(b, &ex);
+  return ldexpf(1.0f, max(-120, min(120, -ex)));
+}
+
+// The first H 2 nkb tiles workgroups (a wave each) take 32 latents of a path (one packed
+// word per output row) of one head for 32 tokens: q' = (h (.) q) U as 32 x 32 tiles,
+// h (.) q cut into three bf16 terms, the signs as bf16 +-1, so every product is exact.
+// The others take the rotary part (and the row's zeros) of one token and kRopeHeads heads.
 template <int DT, int SC, int CD, int TQ>
-__global__ void __launch_bounds__(kAThreads) absorb_kernel(LatentAttnArgs a, char* qout, float* qsc) {
-  __shared__ float hq[2][kMaxHead];
-  __shared__ float qv[kMaxLatentRow];
-  __shared__ float red[kAThreads / 64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H;
+__global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout, float* qsc, int nkb, int n_mma) {
+  const int lane = threadIdx.x, hh = lane >> 5;
   const CacheArgs& c = a.c;
-  const int r = c.r, dn = a.d_nope, dr = c.d_rope, row = c.row;
-  const int n_out = a.Hk * (dn + a.d_v), i0 = h / (a.H / a.Hk) * dn;
-  const char* q = static_cast<const char*>(a.q) + (t * a.q_t + h * a.q_h) * esize<DT>();
-  for (int i = tid; i < 2 * dn; i += kAThreads) {
-    const int p = i >= dn, j = i - p * dn;
-    hq[p][j] = ld<SC>(a.h[p], i0 + j) * ld<DT>(q, j);
+  const int r = c.r, dn = a.d_nope, dr = c.d_rope, row = c.row, G = a.H / a.Hk;
+  constexpr int ES = esize<CD>();
+  if (static_cast<int>(blockIdx.x) < n_mma) {
+    const int u = blockIdx.x % (2 * nkb), hb = blockIdx.x / (2 * nkb), h = hb % a.H, t0 = hb / a.H * kAbsTokens;
+    const int p = u >= nkb, kb = u - p * nkb, i0 = h / G * dn;
+    const PackedView v{static_cast<const uint32_t*>(a.U[p]), a.Hk * (dn + a.d_v), r >> 5, r & 31};
+    const int t = min(t0 + (lane & 31), a.T - 1), bit = lane & 31;
+    const char* q = static_cast<const char*>(a.q) + (t * a.q_t + h * a.q_h) * esize<DT>();
+    floatx16 acc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+    float top = 0.0f, rope = 0.0f;
+    for (int c0 = 0; c0 < dn; c0 += 16) {
+      const int i = c0 + 8 * hh;
+      uint32_t w[8];
+      if (c0 + 16 <= dn) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = load_word(v, kb, i0 + i + e);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = load_word(v, kb, i0 + min(i + e, dn - 1));
+      }
+      float x[8];
+      u32x4 s;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool ok = i + e < dn;
+        const float qe = ld_or0<DT>(q, i + e, ok);
+        x[e] = qe * ld_or0<SC>(a.h[p], i0 + i + e, ok);
+        if constexpr (CD == kDtF16) top = fmaxf(top, fmaxf(fabsf(x[e]), fabsf(qe * ld_or0<SC>(a.h[1 - p], i0 + i + e, ok))));
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s[e] = 0x3f803f80u ^ (((w[2 * e] >> bit) & 1u) << 15) ^ ((w[2 * e + 1] >> bit) << 31);
+      Frag<kDtBF16> sf, xf[3];
+      sf.v[0] = s;
+      to_terms<kDtBF16, 3>(x, xf);
+#pragma unroll
+      for (int n = 0; n < 3; ++n) acc = mma32<kDtBF16>(xf[n], sf, acc);
+    }
+    float f = 1.0f;
+    if constexpr (CD == kDtF16) {
+      for (int i = hh; i < dr; i += 2) rope = fmaxf(rope, fabsf(ld<DT>(q, dn + i)));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      rope = fmaxf(rope, __shfl_xor(rope, 32));
+      f = row_factor(top, rope, dn);
+    }
+    const int k = 32 * kb + bit;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int tt = 8 * (e >> 2) + 4 * hh + (e & 3);
+      float x = acc[e];
+      if constexpr (CD == kDtF16) x *= __shfl(f, tt);
+      if (t0 + tt < a.T && k < r) {
+        char* o = qout + ((static_cast<int64_t>(t0 + tt) * a.H + h) * TQ * row + p * r + k) * ES;
+#pragma unroll
+        for (int n = 0; n < TQ; ++n) {
+          const float y = rounded<CD>(x);
+          st<CD>(o + static_cast<int64_t>(n) * row * ES, 0, y);
+          x -= y;
+        }
+      }
+    }
+    return;
   }
+  const int nh = (a.H + kRopeHeads - 1) / kRopeHeads, id = blockIdx.x - n_mma;
+  const int t = id / nh, h0 = id % nh * kRopeHeads, h1 = min(a.H, h0 + kRopeHeads);
   int pos = 0;
-  if (dr > 0) {
+  if (dr > 0 && a.freqs != nullptr) {
     const int b = seq_of(c, t, a.T, lane);
     if (b >= 0) {
       const SeqWork s = seq_work(c, b, a.T, a.H, 32);
       pos = max(0, s.len - s.nq + (t - s.q0));
     }
   }
-  __syncthreads();
-  float top = 0.0f;
-  for (int k = tid; k < row; k += kAThreads) {
-    float v = 0.0f;
-    if (k < 2 * r) {
-      const int p = k >= r, kk = k - p * r;
-      const PackedView u{static_cast<const uint32_t*>(a.U[p]), n_out, r >> 5, r & 31};
-      const int kb = kk >> 5, sh = 31 - (kk & 31);
-      float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
-      int i = 0;
-      for (; i + 4 <= dn; i += 4) {
-        const uint32_t w0 = load_word(u, kb, i0 + i), w1 = load_word(u, kb, i0 + i + 1);
-        const uint32_t w2 = load_word(u, kb, i0 + i + 2), w3 = load_word(u, kb, i0 + i + 3);
-        s0 += __uint_as_float(__float_as_uint(hq[p][i]) ^ ((w0 << sh) & 0x80000000u));
-        s1 += __uint_as_float(__float_as_uint(hq[p][i + 1]) ^ ((w1 << sh) & 0x80000000u));
-        s2 += __uint_as_float(__float_as_uint(hq[p][i + 2]) ^ ((w2 << sh) & 0x80000000u));
-        s3 += __uint_as_float(__float_as_uint(hq[p][i + 3]) ^ ((w3 << sh) & 0x80000000u));
+  float f[kRopeHeads];
+#pragma unroll
+  for (int n = 0; n < kRopeHeads; ++n) {
+    f[n] = 1.0f;
+    if (h0 + n >= h1) continue;
+    if constexpr (CD == kDtF16) {
+      const char* q = static_cast<const char*>(a.q) + (t * a.q_t + (h0 + n) * a.q_h) * esize<DT>();
+      const int i0 = (h0 + n) / G * dn;
+      float top = 0.0f, rope = 0.0f;
+      for (int i = lane; i < dn; i += 64) {
+        const float qe = ld<DT>(q, i);
+        top = fmaxf(top, fmaxf(fabsf(qe * ld<SC>(a.h[0], i0 + i)), fabsf(qe * ld<SC>(a.h[1], i0 + i))));
       }
-      for (; i < dn; ++i)
-        s0 += __uint_as_float(__float_as_uint(hq[p][i]) ^ ((load_word(u, kb, i0 + i) << sh) & 0x80000000u));
-      v = (s0 + s1) + (s2 + s3);
-    } else if (k < 2 * r + dr) {
-      const int i = k - 2 * r, half = dr / 2;
-      v = ld<DT>(q, dn + i);
-      if (a.freqs != nullptr) {
-        const bool low = i < half;
-        float cs, sn;
-        turn_of(pos, a.freqs[low ? i : i - half], cs, sn);
-        const float o = ld<DT>(q, dn + (low ? i + half : i - half));
-        v = low ? v * cs - o * sn : v * cs + o * sn;
+      for (int i = lane; i < dr; i += 64) rope = fmaxf(rope, fabsf(ld<DT>(q, dn + i)));
+#pragma unroll
+      for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s)), rope = fmaxf(rope, __shfl_xor(rope, s));
+      f[n] = row_factor(top, rope, dn);
+    }
+    if (lane == 0) qsc[static_cast<int64_t>(t) * a.H + h0 + n] = a.scale * kLog2e / f[n];
+  }
+  const int half = dr / 2;
+  for (int i = lane; i < row - 2 * r; i += 64) {
+    const bool in = i < dr, low = i < half;
+    float cs = 1.0f, sn = 0.0f;
+    if (in && a.freqs != nullptr) turn_of(pos, a.freqs[low ? i : i - half], cs, sn);
+    if (low) sn = -sn;
+#pragma unroll
+    for (int n = 0; n < kRopeHeads; ++n) {
+      if (h0 + n >= h1) continue;
+      const char* q = static_cast<const char*>(a.q) + (t * a.q_t + (h0 + n) * a.q_h) * esize<DT>();
+      float x = 0.0f;
+      if (in) {
+        x = ld<DT>(q, dn + i);
+        if (a.freqs != nullptr) x = x * cs + ld<DT>(q, dn + (low ? i + half : i - half)) * sn;
       }
-    }
-    qv[k] = v;
-    top = fmaxf(top, fabsf(v));
-  }
-  float f = 1.0f;
-  if constexpr (CD == kDtF16) {
-    // q' may leave f16's range: rows are brought to a maximum in [1/2, 1) by a power of two
+      x *= f[n];
+      char* o = qout + ((static_cast<int64_t>(t) * a.H + h0 + n) * TQ * row + 2 * r + i) * ES;
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
-    if (lane == 0) red[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    if (top > 0.0f && top < 1e38f) {
-      int ex;
-      frexpf(top, &ex);
-      f = ldexpf(1.0f, max(-120, min(120, -ex)));
-    }
-  }
-  __syncthreads();
-  const int64_t m = static_cast<int64_t>(t) * a.H + h;
-  if (tid == 0) qsc[m] = a.scale * kLog2e / f;
-  char* out = qout + m * TQ * row * esize<CD>();
-  for (int k = 8 * tid; k < row; k += 8 * kAThreads) {
-    float x[8];
-    Frag<CD> fr[TQ];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = qv[k + e] * f;
-    to_terms<CD, TQ>(x, fr);
-#pragma unroll
-    for (int n = 0; n < TQ; ++n) {
-      char* p = out + (n * row + k) * esize<CD>();
-      *reinterpret_cast<u32x4*>(p) = fr[n].v[0];
-      if constexpr (CD == kDtF32) *reinterpret_cast<u32x4*>(p + 16) = fr[n].v[1];
+      for (int m = 0; m < TQ; ++m) {
+        const float y = rounded<CD>(x);
+        st<CD>(o + static_cast<int64_t>(m) * row * ES, 0, y);
+        x -= y;
+      }
     }
   }
 }
@@ -543,8 +603,8 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 #pragma unroll
       for (int sl = 0; sl < 2; ++sl) {
         if (16 * sl >= p.tpt) break;
-        // probabilities in the cache's type: with 16-bit activations one rounding (relative
-        // half a step each, of terms that the output averages), with fp32 ones TP terms
+        // probabilities in terms of the cache's type: one rounding (relative half a step each,
+        // of terms that the output averages) where the output's type is no finer, else TP terms
         float pv[8];
         Frag<CD> pf[TP];
 #pragma unroll
@@ -617,7 +677,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 // ---------------------------------------------------------------------------
 // join
 // ---------------------------------------------------------------------------
-constexpr int kJThreads = 256;
+constexpr int kJThreads = 512;
 
 struct JoinArgs {
   LatentAttnArgs a;
@@ -632,7 +692,7 @@ template <int DT, int SC>
 __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
   __shared__ float wt[256];
   __shared__ __attribute__((aligned(16))) float ov[2][kMaxLatentRank];
-  __shared__ float part[2][kMaxHead];
+  __shared__ float part[2][2][kMaxHead];
   const LatentAttnArgs& a = j.a;
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -678,17 +738,19 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
   const float* po = j.o + (slot0 * kCols + m) * ow;
   for (int k = tid; k < 2 * r; k += kJThreads) {
     float v = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < n; ++i) v += wt[i] * po[static_cast<int64_t>(i) * kCols * ow + k];
     ov[k >= r][k >= r ? k - r : k] = v * inv;
   }
   __syncthreads();
   const int n_out = a.Hk * (a.d_nope + a.d_v), row0 = a.Hk * a.d_nope + h / (a.H / a.Hk) * a.d_v;
-  for (int q = tid; q < 2 * a.d_v; q += kJThreads) {
-    const int p = q >= a.d_v, i = q - p * a.d_v;
+  // a thread per output, path and half of the path's words
+  const int nb2 = (rp / 32 + 1) / 2;
+  for (int q = tid; q < 4 * a.d_v; q += kJThreads) {
+    const int ph = q / a.d_v, p = ph & 1, half = ph >> 1, i = q - ph * a.d_v;
     const PackedView u{static_cast<const uint32_t*>(a.U[p]), n_out, r >> 5, r & 31};
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int kb = 0; kb < rp / 32; ++kb) {
+    for (int kb = half * nb2; kb < (half ? rp / 32 : nb2); ++kb) {
       const uint32_t w = load_word(u, kb, row0 + i);
 #pragma unroll
       for (int k = 0; k < 32; k += 4) {
@@ -699,10 +761,14 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
           s[e] += __uint_as_float(__float_as_uint(vv[e]) ^ ((w << (31 - k - e)) & 0x80000000u));
       }
     }
-    part[p][i] = ld<SC>(a.h[p], row0 + i) * ((s[0] + s[1]) + (s[2] + s[3]));
+    part[half][p][i] = (s[0] + s[1]) + (s[2] + s[3]);
   }
   __syncthreads();
-  for (int i = tid; i < a.d_v; i += kJThreads) st<DT>(out, i, part[0][i] + part[1][i]);
+  for (int i = tid; i < a.d_v; i += kJThreads) {
+    const float y0 = ld<SC>(a.h[0], row0 + i) * (part[0][0][i] + part[1][0][i]);
+    const float y1 = ld<SC>(a.h[1], row0 + i) * (part[0][1][i] + part[1][1][i]);
+    st<DT>(out, i, y0 + y1);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -721,25 +787,32 @@ hipError_t split_cd(const SplitArgs& s, hipStream_t stream) {
   if (s.p.ncw == 1) {
     switch (s.p.upw) {
       case 4: return split_launch<CD, TQ, TP, 4, false>(s, stream);
+      case 6: return split_launch<CD, TQ, TP, 6, false>(s, stream);
       case 8: return split_launch<CD, TQ, TP, 8, false>(s, stream);
+      case 10: return split_launch<CD, TQ, TP, 10, false>(s, stream);
       default: return split_launch<CD, TQ, TP, 12, false>(s, stream);
     }
   }
   switch (s.p.upw) {
     case 4: return split_launch<CD, TQ, TP, 4, true>(s, stream);
+    case 6: return split_launch<CD, TQ, TP, 6, true>(s, stream);
     case 8: return split_launch<CD, TQ, TP, 8, true>(s, stream);
+    case 10: return split_launch<CD, TQ, TP, 10, true>(s, stream);
     default: return split_launch<CD, TQ, TP, 12, true>(s, stream);
   }
 }
 
 template <int DT, int SC, int CD>
 hipError_t run(const LatentAttnArgs& a, hipStream_t stream) {
-  constexpr int TQ = terms_q(CD, DT == kDtF32), TP = terms_p(CD, DT == kDtF32);
+  constexpr int TQ = terms_q(CD, DT == kDtF32), TP = terms_p(CD, DT);
   const LatPlan p = lat_plan(a.c.r, a.c.d_rope, esize<CD>());
   const LatWs w = lat_ws(a.T, a.c.n_seq, a.H, a.c.r, a.c.d_rope);
   char* ws = static_cast<char*>(a.ws);
   float* qsc = reinterpret_cast<float*>(ws + w.qs_off);
-  hipLaunchKernelGGL((absorb_kernel<DT, SC, CD, TQ>), dim3(a.T * a.H), dim3(kAThreads), 0, stream, a, ws, qsc);
+  const int nkb = (a.c.r + 31) / 32;
+  const int n_mma = a.H * 2 * nkb * ((a.T + kAbsTokens - 1) / kAbsTokens);
+  const int n_rope = a.T * ((a.H + kRopeHeads - 1) / kRopeHeads);
+  hipLaunchKernelGGL((absorb_kernel<DT, SC, CD, TQ>), dim3(n_mma + n_rope), dim3(64), 0, stream, a, ws, qsc, nkb, n_mma);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   SplitArgs s{};
