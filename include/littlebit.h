@@ -523,7 +523,8 @@ lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const vo
    query's position (freqs; NULL: taken as they are); out [T x H x d_v]
    contiguous, in act_dtype.  A query that sees no token gets 0.  Only U and h of
    the paths are read (of the fused layer, d_out = Hk (d_nope + d_v)).  H a
-   multiple of Hk; d_nope, d_v <= 256 (LB_ERR_SHAPE); scale finite and > 0
+   multiple of Hk; d_nope, d_v <= 256; (T H / 32 + n_seq) (max_pages page_size / 16
+   + 1) < 2^31 (LB_ERR_SHAPE); scale finite and > 0
    (LB_ERR_ARG).  q' enters the scores with at least 16 significant bits (24 for
    fp32 activations), softmax statistics and sums are fp32; probabilities enter
    the sums rounded to the cache's type where out's is no finer, else in two or

@@ -162,6 +162,8 @@ lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int6
       !strides_ok(q_t, q_h) || !fits(T, H, lb::latent_row(cache->r, cache->d_rope)) ||
       !fits(T, H, d_nope + cache->d_rope) || !fits(T, H, d_v) || !fits(Hk, d_nope + d_v, cache->r))
     return LB_ERR_SHAPE;
+  // the kernels count steps of 16 tokens or more of items of 32 query rows in 31 bits
+  if (!fits(T * H / 32 + cache->n_seq, cache->max_pages * cache->page_size / 16 + 1)) return LB_ERR_SHAPE;
   if (!scale_ok(scale)) return LB_ERR_ARG;
   if (T == 0 || H == 0 || d_v == 0 || cache->n_seq == 0) return LB_OK;
   if (!out || (d_nope + cache->d_rope > 0 && !q)) return LB_ERR_NULL;

@@ -28,6 +28,7 @@ typedef __attribute__((address_space(1))) const void* glb_ptr;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr size_t kLdsMax = 163840;
 constexpr int kCols = 32;  // query rows of an item (columns of the tiles)
+constexpr int kG = 256;    // workgroups of split (one a CU)
 
 // ---------------------------------------------------------------------------
 // plan (host)
@@ -45,7 +46,6 @@ struct LatPlan {
   int rps;     // 16-byte pieces of an LDS row (an odd number of units)
   int tile_bytes, xchg_bytes;
   size_t lds;
-  int G;       // workgroups of split
 };
 
 __host__ LatPlan lat_plan(int r, int d_rope, int es) {
@@ -78,7 +78,6 @@ __host__ LatPlan lat_plan(int r, int d_rope, int es) {
     const size_t red = static_cast<size_t>(p.ntw) * kCols * (p.vu * 32 + 4) * 4 + p.ntw * kCols * 8;
     if (red > p.lds) p.lds = red;
   }
-  p.G = 256;
   return p;
 }
 
@@ -95,7 +94,7 @@ struct LatWs {
 __host__ LatWs lat_ws(int64_t T, int64_t n_seq, int64_t H, int r, int d_rope) {
   LatWs w{};
   const int64_t row = latent_row(r, d_rope), ow = (2 * r + 31) / 32 * 32;
-  const int64_t slots = 256 + (T * H + kCols - 1) / kCols + n_seq;
+  const int64_t slots = kG + (T * H + kCols - 1) / kCols + n_seq;
   auto up = [](size_t b) { return (b + 255) / 256 * 256; };
   w.qs_off = up(static_cast<size_t>(T * H * row) * 6);
   w.ml_off = w.qs_off + up(static_cast<size_t>(T * H) * 4);
@@ -108,7 +107,8 @@ __host__ LatWs lat_ws(int64_t T, int64_t n_seq, int64_t H, int r, int d_rope) {
 // work map: sequence b has ceil(nq_b H / 32) items of ceil(len_b / step) steps each;
 // all W steps in a row are dealt to G workgroups (at most W), g taking [W g / G, W (g + 1) / G);
 // its part of the item numbered i over all sequences goes to slot g + i, so that an
-// item's slots are consecutive and no two meet
+// item's slots are consecutive and no two meet.  Sums stay below 2^31 (the caller's
+// sizes are checked for it).
 // ---------------------------------------------------------------------------
 struct SeqWork {
   int q0, nq;       // first token, tokens
@@ -120,66 +120,110 @@ __device__ __forceinline__ SeqWork seq_work(const CacheArgs& c, int b, int T, in
   int hi;
   seq_range(c.cu, b, T, s.q0, hi);
   s.nq = hi - s.q0;
-  s.len = static_cast<int>(
-      max(int64_t(0), min(static_cast<int64_t>(c.lens[b]), static_cast<int64_t>(c.max_pages) * c.page_size)));
-  s.items = static_cast<int>((static_cast<int64_t>(s.nq) * H + kCols - 1) / kCols);
-  s.steps = (s.len + step - 1) / step;
+  s.len = max(0, min(c.lens[b], c.max_pages * c.page_size));
+  s.items = (s.nq * H + kCols - 1) / kCols;
+  // step is 16, 32, 64 or 128
+  s.steps = (s.len + step - 1) >> (31 - __builtin_clz(step));
   return s;
 }
-__device__ __forceinline__ int64_t wave_scan(int64_t v, int lane) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const int64_t o = __shfl_up(v, s);
-    if (lane >= s) v += o;
-  }
-  return v;
-}
-// all steps of all sequences (every lane)
-__device__ __forceinline__ int64_t total_work(const CacheArgs& c, int T, int H, int step, int lane) {
-  int64_t w = 0;
-  for (int b = lane; b < c.n_seq; b += 64) {
-    const SeqWork s = seq_work(c, b, T, H, step);
-    w += static_cast<int64_t>(s.items) * s.steps;
-  }
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) w += __shfl_xor(w, s);
-  return w;
-}
-// The sequence that `find` picks by (b, first step, first item, its work): the first one
-// with by_step ? start + work > x : b == x.  Returns b (-1: none) and the sums before it.
-__device__ __forceinline__ int find_work(const CacheArgs& c, int T, int H, int step, int lane, bool by_step, int64_t x,
-                                         int64_t& steps_before, int64_t& items_before) {
-  int64_t sb = 0, ib = 0;
-  for (int b0 = 0; b0 < c.n_seq; b0 += 64) {
-    const int b = b0 + lane;
-    int64_t w = 0, it = 0;
-    if (b < c.n_seq) {
-      const SeqWork s = seq_work(c, b, T, H, step);
-      w = static_cast<int64_t>(s.items) * s.steps, it = s.items;
-    }
-    const int64_t ws = wave_scan(w, lane), is = wave_scan(it, lane);
-    const uint64_t m = __ballot(b < c.n_seq && (by_step ? sb + ws > x : b == x));
-    if (m != 0) {
-      const int k = __builtin_ctzll(m);
-      steps_before = sb + __shfl(ws, k) - __shfl(w, k);
-      items_before = ib + __shfl(is, k) - __shfl(it, k);
-      return b0 + k;
-    }
-    sb += __shfl(ws, 63);
-    ib += __shfl(is, 63);
-  }
-  return -1;
+__device__ __forceinline__ SeqWork seq_lane(const SeqWork& s, int k) {
+  SeqWork r;
+  r.q0 = __builtin_amdgcn_readlane(s.q0, k);
+  r.nq = __builtin_amdgcn_readlane(s.nq, k);
+  r.len = __builtin_amdgcn_readlane(s.len, k);
+  r.items = __builtin_amdgcn_readlane(s.items, k);
+  r.steps = __builtin_amdgcn_readlane(s.steps, k);
+  return r;
 }
 
-// the sequence of token t (-1: none)
-__device__ __forceinline__ int seq_of(const CacheArgs& c, int t, int T, int lane) {
-  for (int b0 = 0; b0 < c.n_seq; b0 += 64) {
-    int lo = 0, hi = 0;
-    if (b0 + lane < c.n_seq) seq_range(c.cu, b0 + lane, T, lo, hi);
-    const uint64_t m = __ballot(lo <= t && t < hi);
-    if (m != 0) return b0 + __builtin_ctzll(m);
+// The work map of a wave.  Its lanes hold 64 sequences at a time (the arrays are read
+// once for batches of up to 64).
+struct WorkMap {
+  const CacheArgs& c;
+  int T, H, step, lane;
+  int block = -1;  // the 64 sequences held
+  SeqWork s;
+  int ws, is;      // inclusive sums of steps and items over them
+  __device__ __forceinline__ void hold(int b0) {
+    if (b0 == block) return;
+    block = b0;
+    s = SeqWork{0, 0, 0, 0, 0};
+    if (b0 + lane < c.n_seq) s = seq_work(c, b0 + lane, T, H, step);
+    ws = s.items * s.steps, is = s.items;
+    if (c.n_seq > 1) {
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(ws, d), q = __shfl_up(is, d);
+        if (lane >= d) ws += o, is += q;
+      }
+    }
   }
-  return -1;
+  __device__ __forceinline__ int last() const { return min(63, c.n_seq - 1 - block); }
+  __device__ __forceinline__ int total() {
+    int w = 0;
+    for (int b0 = (c.n_seq - 1) / 64 * 64; b0 >= 0; b0 -= 64) {  // block 0 last: it stays held
+      hold(b0);
+      w += __builtin_amdgcn_readlane(ws, last());
+    }
+    return w;
+  }
+  // The sequence whose steps contain number x (by_step) or whose tokens contain row x:
+  // its index (-1: none), its work, and the steps and items before it.
+  __device__ __forceinline__ int find(bool by_step, int x, SeqWork& out, int& sb, int& ib) {
+    sb = 0, ib = 0;
+    for (int b0 = 0; b0 < c.n_seq; b0 += 64) {
+      hold(b0);
+      const uint64_t m = __ballot(b0 + lane < c.n_seq && (by_step ? sb + ws > x : s.q0 <= x && x < s.q0 + s.nq));
+      if (m != 0) {
+        const int k = __builtin_ctzll(m);
+        out = seq_lane(s, k);
+        sb += __builtin_amdgcn_readlane(ws, k) - out.items * out.steps;
+        ib += __builtin_amdgcn_readlane(is, k) - out.items;
+        return b0 + k;
+      }
+      sb += __builtin_amdgcn_readlane(ws, last());
+      ib += __builtin_amdgcn_readlane(is, last());
+    }
+    return -1;
+  }
+};
+__device__ __forceinline__ int first_step(int W, int g) {
+  return W < kG ? g : static_cast<int>((static_cast<int64_t>(W) * g) >> 8);
+}
+// the workgroup that step x belongs to
+__device__ __forceinline__ int group_of(int W, int x) {
+  if (W < kG) return x;
+  // floor of an exact quotient below 2^8 of integers below 2^40: at least 2^-31 from any wrong one
+  return static_cast<int>(static_cast<double>((static_cast<int64_t>(x) + 1) * kG - 1) / static_cast<double>(W));
+}
+
+// n / d for 0 <= n < 2^31 by a multiplication: m = ceil(2^(31 + l) / d), l = ceil(log2 d) (m = 0: d = 1)
+struct Divisor {
+  uint32_t m, shift;
+  int d;
+};
+__host__ Divisor divisor(int d) {
+  int l = 0;
+  while ((int64_t(1) << l) < d) ++l;
+  if (l == 0) return Divisor{0, 0, 1};
+  return Divisor{static_cast<uint32_t>(((uint64_t(1) << (31 + l)) + d - 1) / d), static_cast<uint32_t>(l - 1), d};
+}
+__device__ __forceinline__ int quotient(int n, const Divisor& d) {
+  return d.m == 0 ? n : static_cast<int>(__umulhi(static_cast<uint32_t>(n), d.m) >> d.shift);
+}
+
+// The words of one word column (latents 32 kb ..) of a packed matrix: full words, or
+// the tail plane's 16- or 32-bit ones.
+struct WordColumn {
+  const char* p;
+  bool half;  // 16-bit words
+};
+__device__ __forceinline__ WordColumn word_column(const void* U, int n_out, int r, int kb) {
+  const int nb = r >> 5, w = r & 31;
+  return WordColumn{static_cast<const char*>(U) + static_cast<int64_t>(4) * min(kb, nb) * n_out, kb >= nb && w <= 16};
+}
+__device__ __forceinline__ uint32_t word_at(const WordColumn& c, int o) {
+  return c.half ? reinterpret_cast<const uint16_t*>(c.p)[o] : reinterpret_cast<const uint32_t*>(c.p)[o];
 }
 
 // x[8] as N terms of type CD, each the rounding of what the previous ones left
@@ -227,7 +271,8 @@ __device__ __forceinline__ float row_factor(float top, float rope, int dn) {
 // h (.) q cut into three bf16 terms, the signs as bf16 +-1, so every product is exact.
 // The others take the rotary part (and the row's zeros) of one token and kRopeHeads heads.
 template <int DT, int SC, int CD, int TQ>
-__global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout, float* qsc, int nkb, int n_mma) {
+__global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout, float* qsc, int nkb, int n_mma,
+                                                   bool vec) {
   const int lane = threadIdx.x, hh = lane >> 5;
   const CacheArgs& c = a.c;
   const int r = c.r, dn = a.d_nope, dr = c.d_rope, row = c.row, G = a.H / a.Hk;
@@ -235,40 +280,63 @@ __global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout
   if (static_cast<int>(blockIdx.x) < n_mma) {
     const int u = blockIdx.x % (2 * nkb), hb = blockIdx.x / (2 * nkb), h = hb % a.H, t0 = hb / a.H * kAbsTokens;
     const int p = u >= nkb, kb = u - p * nkb, i0 = h / G * dn;
-    const PackedView v{static_cast<const uint32_t*>(a.U[p]), a.Hk * (dn + a.d_v), r >> 5, r & 31};
+    const WordColumn v = word_column(a.U[p], a.Hk * (dn + a.d_v), r, kb);
     const int t = min(t0 + (lane & 31), a.T - 1), bit = lane & 31;
     const char* q = static_cast<const char*>(a.q) + (t * a.q_t + h * a.q_h) * esize<DT>();
     floatx16 acc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
     float top = 0.0f, rope = 0.0f;
-    for (int c0 = 0; c0 < dn; c0 += 16) {
-      const int i = c0 + 8 * hh;
-      uint32_t w[8];
-      if (c0 + 16 <= dn) {
+    // 64 inputs at a time: all their loads first
+    for (int c0 = 0; c0 < dn; c0 += 64) {
+      uint32_t w[4][8];
+      Frag<DT> qv[4];
+      Frag<SC> hv[4], h2[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = load_word(v, kb, i0 + i + e);
+      for (int n = 0; n < 4; ++n) {
+        const int i = c0 + 16 * n + 8 * hh;
+        qv[n] = load8<DT>(q, i, dn, vec);
+        hv[n] = load8<SC>(static_cast<const char*>(a.h[p]) + i0 * esize<SC>(), i, dn, vec);
+        if constexpr (CD == kDtF16)
+          h2[n] = load8<SC>(static_cast<const char*>(a.h[1 - p]) + i0 * esize<SC>(), i, dn, vec);
+      }
+      if (v.half) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            w[n][e] = reinterpret_cast<const uint16_t*>(v.p)[i0 + min(c0 + 16 * n + 8 * hh + e, dn - 1)];
+      } else if (c0 + 64 <= dn) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[n][e] = reinterpret_cast<const uint32_t*>(v.p)[i0 + c0 + 16 * n + 8 * hh + e];
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = load_word(v, kb, i0 + min(i + e, dn - 1));
-      }
-      float x[8];
-      u32x4 s;
+        for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool ok = i + e < dn;
-        const float qe = ld_or0<DT>(q, i + e, ok);
-        x[e] = qe * ld_or0<SC>(a.h[p], i0 + i + e, ok);
-        if constexpr (CD == kDtF16) top = fmaxf(top, fmaxf(fabsf(x[e]), fabsf(qe * ld_or0<SC>(a.h[1 - p], i0 + i + e, ok))));
+          for (int e = 0; e < 8; ++e)
+            w[n][e] = reinterpret_cast<const uint32_t*>(v.p)[i0 + min(c0 + 16 * n + 8 * hh + e, dn - 1)];
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        s[e] = 0x3f803f80u ^ (((w[2 * e] >> bit) & 1u) << 15) ^ ((w[2 * e + 1] >> bit) << 31);
-      Frag<kDtBF16> sf, xf[3];
-      sf.v[0] = s;
-      to_terms<kDtBF16, 3>(x, xf);
+      for (int n = 0; n < 4; ++n) {
+        float x[8];
+        u32x4 s;
 #pragma unroll
-      for (int n = 0; n < 3; ++n) acc = mma32<kDtBF16>(xf[n], sf, acc);
+        for (int e = 0; e < 8; ++e) {
+          const float qe = frag_elem<DT>(qv[n], e);
+          x[e] = qe * frag_elem<SC>(hv[n], e);
+          if constexpr (CD == kDtF16) top = fmaxf(top, fmaxf(fabsf(x[e]), fabsf(qe * frag_elem<SC>(h2[n], e))));
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s[e] = 0x3f803f80u ^ (((w[n][2 * e] >> bit) & 1u) << 15) ^ ((w[n][2 * e + 1] >> bit) << 31);
+        Frag<kDtBF16> sf, xf[3];
+        sf.v[0] = s;
+        to_terms<kDtBF16, 3>(x, xf);
+#pragma unroll
+        for (int m = 0; m < 3; ++m) acc = mma32<kDtBF16>(xf[m], sf, acc);
+      }
     }
     float f = 1.0f;
     if constexpr (CD == kDtF16) {
@@ -299,11 +367,10 @@ __global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout
   const int t = id / nh, h0 = id % nh * kRopeHeads, h1 = min(a.H, h0 + kRopeHeads);
   int pos = 0;
   if (dr > 0 && a.freqs != nullptr) {
-    const int b = seq_of(c, t, a.T, lane);
-    if (b >= 0) {
-      const SeqWork s = seq_work(c, b, a.T, a.H, 32);
-      pos = max(0, s.len - s.nq + (t - s.q0));
-    }
+    WorkMap map{c, a.T, a.H, 32, lane};
+    SeqWork s;
+    int sb, ib;
+    if (map.find(false, t, s, sb, ib) >= 0) pos = max(0, s.len - s.nq + (t - s.q0));
   }
   float f[kRopeHeads];
 #pragma unroll
@@ -360,6 +427,7 @@ struct SplitArgs {
   LatPlan p;
   int T, H;
   uint32_t magic;  // lin / rps
+  Divisor page, heads;
   const char* q;
   const float* qsc;
   float* ml;
@@ -425,18 +493,18 @@ __device__ __forceinline__ void wait_loads() {
 template <int CD, int TQ, int TP, int UPW, bool CSPLIT>
 __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  constexpr int PU = 2 * esize<CD>();
+  constexpr int ES = esize<CD>(), PU = 2 * ES;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, ml_ = lane & 31;
   const CacheArgs& c = a.c;
   const LatPlan& p = a.p;
   const int step = p.step;
-  const int64_t W = total_work(c, a.T, a.H, step, lane);
+  WorkMap map{c, a.T, a.H, step, lane};
+  const int W = map.total();
   const int g = blockIdx.x;
-  const int64_t G = min(static_cast<int64_t>(p.G), W);  // no workgroup with a share is without a step
-  if (g >= G) return;
-  int64_t x = W * g / G;
-  const int64_t x_end = W * (g + 1) / G;
+  if (g >= W) return;
+  int x = first_step(W, g);
+  const int x_end = first_step(W, g + 1);
   const int tw = CSPLIT ? 0 : wave, cw = CSPLIT ? wave : 0;
   const int u0 = cw * p.nuw;                                       // the wave's units of the row
   const int nu = max(0, min(p.nuw, p.nu - u0)), vu = max(0, min(nu, p.vu - u0));
@@ -448,24 +516,41 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
   const int ow = p.vu * 32;
 
   while (x < x_end) {
-    int64_t sb, ib;
-    const int b = find_work(c, a.T, a.H, step, lane, true, x, sb, ib);
+    SeqWork sw;
+    int sb, ib;
+    const int b = map.find(true, x, sw, sb, ib);
     if (b < 0) break;
-    const SeqWork sw = seq_work(c, b, a.T, a.H, step);
-    const int item = static_cast<int>((x - sb) / sw.steps);
-    const int s0 = static_cast<int>((x - sb) - static_cast<int64_t>(item) * sw.steps);
-    const int s1 = static_cast<int>(min(static_cast<int64_t>(sw.steps), s0 + (x_end - x)));
+    // (x - sb < items steps, the quotient of 32-bit integers in 64 bits: exact floor)
+    const int item = static_cast<int>(static_cast<double>(x - sb) / static_cast<double>(sw.steps));
+    const int s0 = x - sb - item * sw.steps;
+    const int s1 = min(sw.steps, s0 + (x_end - x));
     const int64_t slot = g + ib + item;
     x += s1 - s0;
 
+    // a token's page; its row of the cache, where the page is one.  Token 0 stands in for
+    // tokens without a place: every row sees it, so that what the masked scores' zero
+    // probabilities are multiplied with is no stranger's infinity.
+    const int32_t* table = c.table + static_cast<int64_t>(b) * c.max_pages;
+    auto page_of = [&](int tok) { return table[quotient(min(tok, sw.len - 1), a.page)]; };
+    auto place = [&](int tok, int page, bool& ok) {
+      ok = tok < sw.len && page >= 0 && page < c.n_pages;
+      return page * c.page_size + (tok - quotient(tok, a.page) * c.page_size);
+    };
+    auto tile_at = [&](int s) { return (s * p.ntw + tw) * p.tpt; };
+    int page = page_of(tile_at(s0) + ml_);
+    const int page0 = table[0];
+
     // the item's query rows: columns of the tiles
     const int rows = sw.nq * a.H;
-    const int rr = min(item * kCols + ml_, rows - 1);
-    const int64_t m_row = static_cast<int64_t>(sw.q0) * a.H + rr;
+    const int rr = min(ml_, rows - 1 - item * kCols);  // within the item
+    const int64_t m0 = static_cast<int64_t>(sw.q0) * a.H + item * kCols;
     const int first = sw.len - sw.nq;  // position of the sequence's first query
-    const int pos = first + rr / a.H;
-    const int pos_min = first + item * kCols / a.H;
-    const float qs = a.qsc[m_row];
+    const int pos = first + quotient(item * kCols + rr, a.heads);
+    const int pos_min = first + quotient(item * kCols, a.heads);
+    const float qs = a.qsc[m0 + rr];
+    const char* qbase = a.q + m0 * TQ * row_bytes + u0 * 32 * ES;
+    const rsrc_t qr = make_rsrc_uniform(qbase, kCols * TQ * static_cast<uint32_t>(row_bytes));
+    const uint32_t qo = rr * TQ * static_cast<uint32_t>(row_bytes) + 8 * hh * ES;
     Frag<CD> qf[2 * UPW][TQ];
 #pragma unroll
     for (int k = 0; k < 2 * UPW; ++k) {
@@ -473,28 +558,18 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
       for (int n = 0; n < TQ; ++n) {
         qf[k][n] = frag_zero<CD>();
         if (k < 2 * nu) {
-          const char* src = a.q + ((m_row * TQ + n) * c.row + 32 * u0 + 16 * k + 8 * hh) * esize<CD>();
-          qf[k][n].v[0] = *reinterpret_cast<const u32x4*>(src);
-          if constexpr (CD == kDtF32) qf[k][n].v[1] = *reinterpret_cast<const u32x4*>(src + 16);
+          const uint32_t so = n * static_cast<uint32_t>(row_bytes);
+          qf[k][n].v[0] = __builtin_amdgcn_raw_buffer_load_b128(qr, qo + 16 * k * ES, so, 0);
+          if constexpr (CD == kDtF32) qf[k][n].v[1] = __builtin_amdgcn_raw_buffer_load_b128(qr, qo + 16 * k * ES + 16, so, 0);
         }
       }
     }
-    // a token's page; its row of the cache, where the page is one.  Token 0 stands in for
-    // tokens without a place: every row sees it, so that what the masked scores' zero
-    // probabilities are multiplied with is no stranger's infinity.
-    auto page_of = [&](int tok) {
-      return c.table[static_cast<int64_t>(b) * c.max_pages + min(tok, sw.len - 1) / c.page_size];
-    };
-    auto place = [&](int tok, int page, bool& ok) {
-      ok = tok < sw.len && page >= 0 && page < c.n_pages;
-      return page * c.page_size + tok % c.page_size;
-    };
     bool ok0;
-    const int at0 = place(0, page_of(0), ok0);
+    const int at0 = place(0, page0, ok0);
     const int place0 = ok0 ? at0 : 0;
-    auto issue = [&](int tok, int page, char* dst) -> uint32_t {
+    auto issue = [&](int tok, int pg, char* dst) -> uint32_t {
       bool ok;
-      const int at = place(tok, page, ok);
+      const int at = place(tok, pg, ok);
       const int idx = ok ? at : place0;
       ok = ok && ml_ < p.tpt;
       for (int i = 0; i < n_ld; ++i) {
@@ -513,9 +588,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[u][e] = 0.0f;
     float mx = -INFINITY, sum = 0.0f;
-    auto tile_at = [&](int s) { return (s * p.ntw + tw) * p.tpt; };
     uint32_t okm = 0, okn = 0;
-    int page = page_of(tile_at(s0) + ml_);
     __syncthreads();  // the previous item's readers of this memory are done
     if (p.stages == 2) {
       okm = issue(tile_at(s0) + ml_, page, tiles);
@@ -654,21 +727,33 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
       }
       if (hh == 0) rml[(wave * kCols + ml_) * 2] = mx, rml[(wave * kCols + ml_) * 2 + 1] = sum;
       __syncthreads();
-      const int nq4 = ow / 4;
-      for (int i = tid; i < kCols * nq4; i += 64 * p.ntw) {
-        const int m = i / nq4, cq = i - m * nq4;
-        float top = -INFINITY;
-        for (int w = 0; w < p.ntw; ++w) top = fmaxf(top, rml[(w * kCols + m) * 2]);
+      // thread: query row m, every eighth (fourth with two waves) group of four columns
+      const int tpr = 2 * p.ntw, m = tid / tpr, cq0 = tid - m * tpr;
+      float top = -INFINITY, f[4], l = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        f[w] = w < p.ntw ? rml[(w * kCols + m) * 2] : -INFINITY;
+        top = fmaxf(top, f[w]);
+      }
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        f[w] = f[w] == -INFINITY ? 0.0f : exp2f(f[w] - top);
+        if (w < p.ntw) l += f[w] * rml[(w * kCols + m) * 2 + 1];
+      }
+      if (cq0 == 0) *reinterpret_cast<float2*>(pm + 2 * m) = make_float2(top, l);
+      const int ws = kCols * st;
+      const float* rm = red + m * st;
+#pragma unroll 2
+      for (int cq = cq0; cq < ow / 4; cq += tpr) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        float l = 0.0f;
-        for (int w = 0; w < p.ntw; ++w) {
-          const float f = top == -INFINITY ? 0.0f : exp2f(rml[(w * kCols + m) * 2] - top);
-          const float4 t = *reinterpret_cast<const float4*>(red + (w * kCols + m) * st + 4 * cq);
-          v.x += f * t.x, v.y += f * t.y, v.z += f * t.z, v.w += f * t.w;
-          l += f * rml[(w * kCols + m) * 2 + 1];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if (w < p.ntw) {
+            const float4 t = *reinterpret_cast<const float4*>(rm + w * ws + 4 * cq);
+            v.x += f[w] * t.x, v.y += f[w] * t.y, v.z += f[w] * t.z, v.w += f[w] * t.w;
+          }
         }
         *reinterpret_cast<float4*>(po + m * ow + 4 * cq) = v;
-        if (cq == 0) pm[2 * m] = top, pm[2 * m + 1] = l;
       }
     }
   }
@@ -677,7 +762,6 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 // ---------------------------------------------------------------------------
 // join
 // ---------------------------------------------------------------------------
-constexpr int kJThreads = 512;
 
 struct JoinArgs {
   LatentAttnArgs a;
@@ -688,7 +772,7 @@ struct JoinArgs {
 
 // A workgroup per (token, head): the partial sums of its row, in workgroup order,
 // then its head's rows of U with h.
-template <int DT, int SC>
+template <int DT, int SC, int kMaxHalf, int kJThreads>
 __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
   __shared__ float wt[256];
   __shared__ __attribute__((aligned(16))) float ov[2][kMaxLatentRank];
@@ -697,23 +781,33 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63;
   const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H;
-  const int b = seq_of(c, t, a.T, lane);
-  if (b < 0) return;  // a row behind the last sequence
   const int step = j.p.step, r = c.r, rp = (r + 31) & ~31;
-  const SeqWork sw = seq_work(c, b, a.T, a.H, step);
+  // the words of this thread's output, path and half of the path's words: they do not
+  // depend on the sums
+  const int n_out = a.Hk * (a.d_nope + a.d_v), row0 = a.Hk * a.d_nope + h / (a.H / a.Hk) * a.d_v;
+  const int nb2 = (rp / 32 + 1) / 2;
+  uint32_t words[kMaxHalf];
+  const int ph = tid / a.d_v, wp = ph & 1, wi = tid - ph * a.d_v, wk = (ph >> 1) * nb2;
+#pragma unroll
+  for (int n = 0; n < kMaxHalf; ++n) {
+    // (the last one may be of 16 bits; absent ones read the first word again)
+    const bool ok = ph < 4 && n < nb2 && wk + n < rp / 32;
+    words[n] = word_at(word_column(a.U[wp], n_out, r, ok ? wk + n : 0), ok ? row0 + wi : 0);
+  }
+  WorkMap map{c, a.T, a.H, step, lane};
+  const int W = map.total();
+  SeqWork sw;
+  int sb, ib;
+  if (map.find(false, t, sw, sb, ib) < 0) return;  // a row behind the last sequence
+#pragma unroll
+  for (int n = 0; n < kMaxHalf; ++n) pin(words[n]);  // (loaded above, not where they are used)
   char* out = static_cast<char*>(a.out) + (static_cast<int64_t>(t) * a.H + h) * a.d_v * esize<DT>();
   if (sw.steps == 0) {
     for (int i = tid; i < a.d_v; i += kJThreads) st<DT>(out, i, 0.0f);
     return;
   }
-  const int64_t W = total_work(c, a.T, a.H, step, lane);
-  int64_t sb = 0, ib = 0;
-  find_work(c, a.T, a.H, step, lane, false, b, sb, ib);
   const int rr = (t - sw.q0) * a.H + h, item = rr / kCols, m = rr - item * kCols;
-  const int64_t x0 = sb + static_cast<int64_t>(item) * sw.steps;
-  const int64_t G = min(static_cast<int64_t>(j.p.G), W);
-  const int g0 = static_cast<int>(((x0 + 1) * G - 1) / W), g1 = static_cast<int>(((x0 + sw.steps) * G - 1) / W);
-  const int n = g1 - g0 + 1;  // <= G
+  const int x0 = sb + item * sw.steps, g0 = group_of(W, x0), n = group_of(W, x0 + sw.steps - 1) - g0 + 1;  // n <= kG
   const int64_t slot0 = g0 + ib + item;
   const int ow = j.p.vu * 32;
   float top = -INFINITY;
@@ -743,25 +837,21 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
     ov[k >= r][k >= r ? k - r : k] = v * inv;
   }
   __syncthreads();
-  const int n_out = a.Hk * (a.d_nope + a.d_v), row0 = a.Hk * a.d_nope + h / (a.H / a.Hk) * a.d_v;
-  // a thread per output, path and half of the path's words
-  const int nb2 = (rp / 32 + 1) / 2;
-  for (int q = tid; q < 4 * a.d_v; q += kJThreads) {
-    const int ph = q / a.d_v, p = ph & 1, half = ph >> 1, i = q - ph * a.d_v;
-    const PackedView u{static_cast<const uint32_t*>(a.U[p]), n_out, r >> 5, r & 31};
+  if (ph < 4) {
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int kb = half * nb2; kb < (half ? rp / 32 : nb2); ++kb) {
-      const uint32_t w = load_word(u, kb, row0 + i);
+#pragma unroll
+    for (int n = 0; n < kMaxHalf; ++n) {
+      if (n >= nb2 || wk + n >= rp / 32) break;
 #pragma unroll
       for (int k = 0; k < 32; k += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(&ov[p][32 * kb + k]);
+        const float4 v = *reinterpret_cast<const float4*>(&ov[wp][32 * (wk + n) + k]);
         const float vv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          s[e] += __uint_as_float(__float_as_uint(vv[e]) ^ ((w << (31 - k - e)) & 0x80000000u));
+          s[e] += __uint_as_float(__float_as_uint(vv[e]) ^ ((words[n] << (31 - k - e)) & 0x80000000u));
       }
     }
-    part[half][p][i] = (s[0] + s[1]) + (s[2] + s[3]);
+    part[ph >> 1][wp][wi] = (s[0] + s[1]) + (s[2] + s[3]);
   }
   __syncthreads();
   for (int i = tid; i < a.d_v; i += kJThreads) {
@@ -779,7 +869,7 @@ hipError_t split_launch(const SplitArgs& s, hipStream_t stream) {
   static LdsLimit limit;
   const hipError_t e = raise_lds(reinterpret_cast<const void*>(&split_kernel<CD, TQ, TP, UPW, CS>), s.p.lds, limit);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((split_kernel<CD, TQ, TP, UPW, CS>), dim3(s.p.G), dim3(64 * s.p.ncw * s.p.ntw), s.p.lds, stream, s);
+  hipLaunchKernelGGL((split_kernel<CD, TQ, TP, UPW, CS>), dim3(kG), dim3(64 * s.p.ncw * s.p.ntw), s.p.lds, stream, s);
   return hipGetLastError();
 }
 template <int CD, int TQ, int TP>
@@ -802,6 +892,12 @@ hipError_t split_cd(const SplitArgs& s, hipStream_t stream) {
   }
 }
 
+template <int DT, int SC, int HALF, int THREADS>
+hipError_t join_launch(const JoinArgs& j, hipStream_t stream) {
+  hipLaunchKernelGGL((join_kernel<DT, SC, HALF, THREADS>), dim3(j.a.T * j.a.H), dim3(THREADS), 0, stream, j);
+  return hipGetLastError();
+}
+
 template <int DT, int SC, int CD>
 hipError_t run(const LatentAttnArgs& a, hipStream_t stream) {
   constexpr int TQ = terms_q(CD, DT == kDtF32), TP = terms_p(CD, DT);
@@ -811,8 +907,11 @@ hipError_t run(const LatentAttnArgs& a, hipStream_t stream) {
   float* qsc = reinterpret_cast<float*>(ws + w.qs_off);
   const int nkb = (a.c.r + 31) / 32;
   const int n_mma = a.H * 2 * nkb * ((a.T + kAbsTokens - 1) / kAbsTokens);
+  auto al = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
+  const bool vec = a.d_nope % 8 == 0 && al(a.q) && al(a.h[0]) && al(a.h[1]) && a.q_t % 8 == 0 && a.q_h % 8 == 0;
   const int n_rope = a.T * ((a.H + kRopeHeads - 1) / kRopeHeads);
-  hipLaunchKernelGGL((absorb_kernel<DT, SC, CD, TQ>), dim3(n_mma + n_rope), dim3(64), 0, stream, a, ws, qsc, nkb, n_mma);
+  hipLaunchKernelGGL((absorb_kernel<DT, SC, CD, TQ>), dim3(n_mma + n_rope), dim3(64), 0, stream, a, ws, qsc, nkb, n_mma,
+                     vec);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   SplitArgs s{};
@@ -820,14 +919,18 @@ hipError_t run(const LatentAttnArgs& a, hipStream_t stream) {
   s.p = p;
   s.T = a.T, s.H = a.H;
   s.magic = static_cast<uint32_t>(((uint64_t(1) << 32) + p.rps - 1) / p.rps);
+  s.page = divisor(a.c.page_size), s.heads = divisor(a.H);
   s.q = ws, s.qsc = qsc;
   s.ml = reinterpret_cast<float*>(ws + w.ml_off);
   s.o = reinterpret_cast<float*>(ws + w.o_off);
   e = split_cd<CD, TQ, TP>(s, stream);
   if (e != hipSuccess) return e;
   JoinArgs j{a, p, s.ml, s.o};
-  hipLaunchKernelGGL((join_kernel<DT, SC>), dim3(a.T * a.H), dim3(kJThreads), 0, stream, j);
-  return hipGetLastError();
+  // four threads an output, and the words of half a path in registers
+  const bool wide = a.d_v > 128, high = a.c.r > 256;
+  if (wide)
+    return high ? join_launch<DT, SC, 12, 1024>(j, stream) : join_launch<DT, SC, 4, 1024>(j, stream);
+  return high ? join_launch<DT, SC, 12, 512>(j, stream) : join_launch<DT, SC, 4, 512>(j, stream);
 }
 template <int DT, int SC>
 hipError_t run_sc(const LatentAttnArgs& a, hipStream_t stream) {
