@@ -43,10 +43,12 @@ struct LatPlan {
   int stages;  // tiles in LDS per wave
   int tpt;     // tokens of a tile (32, or 16 where 32 do not fit)
   int step;    // tokens of a step: tpt ntw
-  int rps;     // 16-byte pieces of an LDS row (an odd number of units)
   int tile_bytes, xchg_bytes;
   size_t lds;
 };
+
+// LDS of ntw waves' sums (rows padded by 16 bytes) and statistics
+__host__ size_t sums_bytes(int ntw, int vu) { return static_cast<size_t>(ntw) * kCols * ((vu * 32 + 4) * 4 + 8); }
 
 __host__ LatPlan lat_plan(int r, int d_rope, int es) {
   LatPlan p{};
@@ -56,13 +58,11 @@ __host__ LatPlan lat_plan(int r, int d_rope, int es) {
   p.ncw = p.nu <= 12 ? 1 : 4;
   p.nuw = (p.nu + p.ncw - 1) / p.ncw;
   p.upw = p.nuw <= 4 ? 4 : (p.nuw + 1) / 2 * 2;
-  const int pu = es * 2;
-  p.rps = pu * (p.nuw | 1);
   p.tpt = 32;
-  p.tile_bytes = 32 * 16 * p.rps;
+  p.tile_bytes = p.nuw * 32 * 32 * es;
   if (p.ncw == 1) {
-    // as many token waves as two tiles each leave room for
-    p.ntw = 8 * static_cast<size_t>(p.tile_bytes) <= kLdsMax ? 4 : 2;
+    // as many token waves as leave room for two tiles each, and for their sums
+    p.ntw = 8 * static_cast<size_t>(p.tile_bytes) <= kLdsMax && sums_bytes(4, p.vu) <= kLdsMax ? 4 : 2;
     p.stages = 2 * static_cast<size_t>(p.ntw) * p.tile_bytes <= kLdsMax ? 2 : 1;
   } else {
     p.ntw = 1;
@@ -75,7 +75,7 @@ __host__ LatPlan lat_plan(int r, int d_rope, int es) {
   p.lds = static_cast<size_t>(nw) * p.stages * p.tile_bytes + p.xchg_bytes;
   if (p.ncw == 1) {
     // the token waves' sums are added through the same memory
-    const size_t red = static_cast<size_t>(p.ntw) * kCols * (p.vu * 32 + 4) * 4 + p.ntw * kCols * 8;
+    const size_t red = sums_bytes(p.ntw, p.vu);
     if (red > p.lds) p.lds = red;
   }
   return p;
@@ -105,7 +105,7 @@ __host__ LatWs lat_ws(int64_t T, int64_t n_seq, int64_t H, int r, int d_rope) {
 
 // ---------------------------------------------------------------------------
 // work map: sequence b has ceil(nq_b H / 32) items of ceil(len_b / step) steps each;
-// all W steps in a row are dealt to G workgroups (at most W), g taking [W g / G, W (g + 1) / G);
+// all W steps in a row are dealt to G workgroups (G <= W), g taking [W g / G, W (g + 1) / G);
 // its part of the item numbered i over all sequences goes to slot g + i, so that an
 // item's slots are consecutive and no two meet.  Sums stay below 2^31 (the caller's
 // sizes are checked for it).
@@ -187,14 +187,20 @@ struct WorkMap {
     return -1;
   }
 };
-__device__ __forceinline__ int first_step(int W, int g) {
-  return W < kG ? g : static_cast<int>((static_cast<int64_t>(W) * g) >> 8);
+// Workgroups that W steps are dealt to: at least 128 tokens each, since a share's
+// partial result (32 rows of 4-byte sums, written and read again) costs as much memory
+// traffic as 128 tokens of a 16-bit cache.
+__device__ __forceinline__ int groups_of(int W, int step) {
+  return max(1, min(kG, W / max(1, 128 / step)));
+}
+// (quotients of integers below 2^40 in 64 bits: a floor is exact, the nearest wrong
+// integer being 2^-31 or more away)
+__device__ __forceinline__ int first_step(int W, int g, int G) {
+  return static_cast<int>(static_cast<double>(static_cast<int64_t>(W) * g) / static_cast<double>(G));
 }
 // the workgroup that step x belongs to
-__device__ __forceinline__ int group_of(int W, int x) {
-  if (W < kG) return x;
-  // floor of an exact quotient below 2^8 of integers below 2^40: at least 2^-31 from any wrong one
-  return static_cast<int>(static_cast<double>((static_cast<int64_t>(x) + 1) * kG - 1) / static_cast<double>(W));
+__device__ __forceinline__ int group_of(int W, int x, int G) {
+  return static_cast<int>(static_cast<double>((static_cast<int64_t>(x) + 1) * G - 1) / static_cast<double>(W));
 }
 
 // n / d for 0 <= n < 2^31 by a multiplication: m = ceil(2^(31 + l) / d), l = ceil(log2 d) (m = 0: d = 1)
@@ -426,7 +432,6 @@ struct SplitArgs {
   CacheArgs c;
   LatPlan p;
   int T, H;
-  uint32_t magic;  // lin / rps
   Divisor page, heads;
   const char* q;
   const float* qsc;
@@ -434,49 +439,52 @@ struct SplitArgs {
   float* o;
 };
 
-// An LDS tile holds 32 tokens' columns of one wave, rows of rps pieces (16 bytes);
-// piece q of row t stands at q with its place in the unit exchanged by swz(t), which
-// with an odd number of units a row makes the row-wise reads free of bank conflicts
-// and the transposed ones even.
+// An LDS tile holds its tokens' columns of one wave, unit by unit: a unit's rows of PU
+// 16-byte pieces (4; fp32: 8), piece q of row t at q ^ swz(t).  Row-wise reads (16
+// rows at one piece) then meet 16 different slots of the 64 banks, transposed reads
+// (8 rows of 4 pieces) each slot twice, the least; and a lane loads the same one or
+// two places of every unit, 64 bytes of a row by four lanes.
 template <int CD>
 __device__ __forceinline__ int swz(int t) {
   return CD == kDtF32 ? (t >> 1) & 7 : (t >> 2) & 3;
 }
+// row t (of tpt) at columns 16 chunk + 8 (lane / 32) ..
 template <int CD>
-__device__ __forceinline__ Frag<CD> tile_rows(const char* t, int rps, int chunk, int lane, int tpt) {
+__device__ __forceinline__ Frag<CD> tile_rows(const char* tile, int tpt, int chunk, int lane) {
   constexpr int PU = 2 * esize<CD>();
-  const int row = lane & (tpt - 1), s = swz<CD>(row);
-  const char* p = t + row * rps * 16;
+  const int t = lane & (tpt - 1), s = swz<CD>(t);
+  const char* p = tile + ((chunk >> 1) * tpt + t) * PU * 16;
   Frag<CD> f;
   if constexpr (CD == kDtF32) {
-    const int q = 4 * chunk + 2 * (lane >> 5);  // two pieces
-    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * ((q & ~(PU - 1)) | ((q ^ s) & (PU - 1))));
-    f.v[1] = *reinterpret_cast<const u32x4*>(p + 16 * ((q & ~(PU - 1)) | (((q + 1) ^ s) & (PU - 1))));
+    const int q = 4 * (chunk & 1) + 2 * (lane >> 5);
+    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * (q ^ s));
+    f.v[1] = *reinterpret_cast<const u32x4*>(p + 16 * ((q + 1) ^ s));
   } else {
-    const int q = 2 * chunk + (lane >> 5);
-    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * ((q & ~(PU - 1)) | ((q ^ s) & (PU - 1))));
+    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * ((2 * (chunk & 1) + (lane >> 5)) ^ s));
   }
   return f;
 }
 // columns 32 u + lane % 32 at the 16 tokens of slice s (slots as in attn_common.h)
 template <int CD>
-__device__ __forceinline__ Frag<CD> tile_cols(const char* t, int rps, int s, int u, int lane) {
+__device__ __forceinline__ Frag<CD> tile_cols(const char* tile, int tpt, int s, int u, int lane) {
+  constexpr int PU = 2 * esize<CD>();
   Frag<CD> f;
   const int hh = lane >> 5;
+  const char* t = tile + u * tpt * PU * 16;
   if constexpr (CD == kDtF32) {
     const int q = (lane & 31) >> 2;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int row = 16 * s + 8 * (k >> 2) + 4 * hh + (k & 3);
-      f.v[k >> 2][k & 3] = *reinterpret_cast<const uint32_t*>(t + row * rps * 16 + 16 * (8 * u + (q ^ swz<CD>(row))) +
-                                                              4 * (lane & 3));
+      f.v[k >> 2][k & 3] =
+          *reinterpret_cast<const uint32_t*>(t + row * PU * 16 + 16 * (q ^ swz<CD>(row)) + 4 * (lane & 3));
     }
   } else {
     typedef __attribute__((address_space(3))) s16x4* lds4;
     const int i = lane & 15, q = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
     const int row = 16 * s + 4 * hh + (i >> 2);
-    const char* p0 = t + row * rps * 16 + 16 * (4 * u + (q ^ swz<CD>(row))) + 8 * (i & 1);
-    const char* p1 = t + (row + 8) * rps * 16 + 16 * (4 * u + (q ^ swz<CD>(row + 8))) + 8 * (i & 1);
+    const char* p0 = t + row * PU * 16 + 16 * (q ^ swz<CD>(row)) + 8 * (i & 1);
+    const char* p1 = t + (row + 8) * PU * 16 + 16 * (q ^ swz<CD>(row + 8)) + 8 * (i & 1);
     const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0)));
     const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1)));
     f.v[0] = u32x4{a[0], a[1], b[0], b[1]};
@@ -484,6 +492,12 @@ __device__ __forceinline__ Frag<CD> tile_cols(const char* t, int rps, int s, int
   return f;
 }
 
+// a barrier for LDS: loads from memory stay in flight
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0xf70);  // vmcnt(0); LDS and scalar counters left alone
@@ -502,15 +516,15 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
   WorkMap map{c, a.T, a.H, step, lane};
   const int W = map.total();
   const int g = blockIdx.x;
-  if (g >= W) return;
-  int x = first_step(W, g);
-  const int x_end = first_step(W, g + 1);
+  const int G = groups_of(W, step);
+  if (W == 0 || g >= G) return;
+  const int x_begin = first_step(W, g, G), x_end = first_step(W, g + 1, G);
+  int x = x_begin;
   const int tw = CSPLIT ? 0 : wave, cw = CSPLIT ? wave : 0;
   const int u0 = cw * p.nuw;                                       // the wave's units of the row
   const int nu = max(0, min(p.nuw, p.nu - u0)), vu = max(0, min(nu, p.vu - u0));
   char* tiles = smem + wave * p.stages * p.tile_bytes;
   float* xchg = reinterpret_cast<float*>(smem + (CSPLIT ? 4 : p.ntw) * p.stages * p.tile_bytes);
-  const int n_ld = p.rps * p.tpt / 64;
   const int64_t row_bytes = static_cast<int64_t>(c.row) * esize<CD>();
   const char* data = static_cast<const char*>(c.data) + u0 * 32 * esize<CD>();
   const int ow = p.vu * 32;
@@ -525,7 +539,6 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
     const int s0 = x - sb - item * sw.steps;
     const int s1 = min(sw.steps, s0 + (x_end - x));
     const int64_t slot = g + ib + item;
-    x += s1 - s0;
 
     // a token's page; its row of the cache, where the page is one.  Token 0 stands in for
     // tokens without a place: every row sees it, so that what the masked scores' zero
@@ -539,6 +552,45 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
     auto tile_at = [&](int s) { return (s * p.ntw + tw) * p.tpt; };
     int page = page_of(tile_at(s0) + ml_);
     const int page0 = table[0];
+
+    bool ok0;
+    const int at0 = place(0, page0, ok0);
+    const int place0 = ok0 ? at0 : 0;
+    // A tile's loads, 64 / PU tokens each: lane l takes piece l % PU of rows l / PU + n 64 / PU.
+    // Returns which of the tile's tokens are seen.
+    constexpr int TPL = 64 / PU, NL = 32 / TPL;  // tokens of a load, loads of a unit of 32 tokens
+    auto issue = [&](int tok, int pg, char* dst) -> uint32_t {
+      bool ok;
+      const int at = place(tok, pg, ok);
+      const int idx = ok ? at : place0;
+      ok = ok && ml_ < p.tpt;
+      const char* src[NL];
+#pragma unroll
+      for (int n = 0; n < NL; ++n) {
+        const int t = lane / PU + n * TPL;
+        src[n] = data + __shfl(idx, t & (p.tpt - 1)) * row_bytes + 16 * ((lane & (PU - 1)) ^ swz<CD>(t));
+      }
+#pragma unroll
+      for (int u = 0; u < UPW; ++u) {
+        if (u < nu) {
+#pragma unroll
+          for (int n = 0; n < NL; ++n) {
+            if (n * TPL < p.tpt)
+              __builtin_amdgcn_global_load_lds((glb_ptr)(src[n] + u * 32 * ES),
+                                               (lds_ptr)(dst + (u * p.tpt + n * TPL) * PU * 16), 16, 0, 0);
+          }
+        }
+      }
+      return static_cast<uint32_t>(__ballot(ok));  // lanes 0 .. 31: the tile's tokens
+    };
+
+    uint32_t okm = 0, okn = 0;
+    if (x > x_begin) lds_barrier();  // the previous item's readers of this memory are done
+    x += s1 - s0;
+    if (p.stages == 2) {
+      okm = issue(tile_at(s0) + ml_, page, tiles);
+      page = page_of(tile_at(s0 + 1) + ml_);
+    }
 
     // the item's query rows: columns of the tiles
     const int rows = sw.nq * a.H;
@@ -564,36 +616,12 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
         }
       }
     }
-    bool ok0;
-    const int at0 = place(0, page0, ok0);
-    const int place0 = ok0 ? at0 : 0;
-    auto issue = [&](int tok, int pg, char* dst) -> uint32_t {
-      bool ok;
-      const int at = place(tok, pg, ok);
-      const int idx = ok ? at : place0;
-      ok = ok && ml_ < p.tpt;
-      for (int i = 0; i < n_ld; ++i) {
-        const uint32_t lin = 64 * i + lane;
-        const int t = __umulhi(lin, a.magic), q = lin - t * p.rps;
-        const int piece = q < PU * nu ? (q & ~(PU - 1)) | ((q ^ swz<CD>(t)) & (PU - 1)) : 0;
-        const char* src = data + __shfl(idx, t) * row_bytes + 16 * piece;
-        __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(dst + 1024 * i), 16, 0, 0);
-      }
-      return static_cast<uint32_t>(__ballot(ok));  // lanes 0 .. 31: the tile's tokens
-    };
-
     floatx16 o[UPW];
 #pragma unroll
     for (int u = 0; u < UPW; ++u)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[u][e] = 0.0f;
     float mx = -INFINITY, sum = 0.0f;
-    uint32_t okm = 0, okn = 0;
-    __syncthreads();  // the previous item's readers of this memory are done
-    if (p.stages == 2) {
-      okm = issue(tile_at(s0) + ml_, page, tiles);
-      page = page_of(tile_at(s0 + 1) + ml_);
-    }
     for (int s = s0; s < s1; ++s) {
       char* tile = tiles;
       if (p.stages == 2) {
@@ -616,7 +644,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 #pragma unroll
       for (int k = 0; k < 2 * UPW; ++k) {
         if (k < 2 * nu) {
-          const Frag<CD> kf = tile_rows<CD>(tile, p.rps, k, lane, p.tpt);
+          const Frag<CD> kf = tile_rows<CD>(tile, p.tpt, k, lane);
 #pragma unroll
           for (int n = 0; n < TQ; ++n) acc = mma32<CD>(kf, qf[k][n], acc);
         }
@@ -628,7 +656,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
         for (int e = 0; e < 16; e += 4)
           *reinterpret_cast<float4*>(xb + wave * 1024 + (e >> 2) * 256 + lane * 4) =
               make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
-        __syncthreads();
+        lds_barrier();
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
           float4 t = *reinterpret_cast<const float4*>(xb + (e >> 2) * 256 + lane * 4);
@@ -686,7 +714,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 #pragma unroll
         for (int u = 0; u < UPW; ++u) {
           if (u < vu) {
-            const Frag<CD> vf = tile_cols<CD>(tile, p.rps, sl, u, lane);
+            const Frag<CD> vf = tile_cols<CD>(tile, p.tpt, sl, u, lane);
 #pragma unroll
             for (int n = 0; n < TP; ++n) o[u] = mma32<CD>(vf, pf[n], o[u]);
           }
@@ -807,7 +835,8 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
     return;
   }
   const int rr = (t - sw.q0) * a.H + h, item = rr / kCols, m = rr - item * kCols;
-  const int x0 = sb + item * sw.steps, g0 = group_of(W, x0), n = group_of(W, x0 + sw.steps - 1) - g0 + 1;  // n <= kG
+  const int x0 = sb + item * sw.steps, G = groups_of(W, step);
+  const int g0 = group_of(W, x0, G), n = group_of(W, x0 + sw.steps - 1, G) - g0 + 1;  // n <= kG
   const int64_t slot0 = g0 + ib + item;
   const int ow = j.p.vu * 32;
   float top = -INFINITY;
@@ -918,7 +947,6 @@ hipError_t run(const LatentAttnArgs& a, hipStream_t stream) {
   s.c = a.c;
   s.p = p;
   s.T = a.T, s.H = a.H;
-  s.magic = static_cast<uint32_t>(((uint64_t(1) << 32) + p.rps - 1) / p.rps);
   s.page = divisor(a.c.page_size), s.heads = divisor(a.H);
   s.q = ws, s.qsc = qsc;
   s.ml = reinterpret_cast<float*>(ws + w.ml_off);
