@@ -22,6 +22,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -164,19 +165,18 @@ def load_library(path: str = LIB_PATH):
     lib.lb_rotate.restype = i32
     lib.lb_rotate.argtypes = [vp, i32, i64, i64, i64, i64, i64, vp, vp, i32, vp, i64, i64, vp]
     lib.lb_latent_append.restype = i32
-    lib.lb_latent_append.argtypes = [ctypes.POINTER(lb_latent_cache), vp, vp, i64, i32, i64, vp, vp]
+    # (structures by address: the binding packs them as bytes, which takes a third of a ctypes object's time)
+    lib.lb_latent_append.argtypes = [vp, vp, vp, i64, i32, i64, vp, vp]
     lib.lb_latent_attention_workspace_bytes.restype = sz
     lib.lb_latent_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
     lib.lb_latent_attention.restype = i32
-    lib.lb_latent_attention.argtypes = [vp, i32, i64, i64, i64, i64, i64, i64, i64, ctypes.POINTER(lb_path), i32,
-                                        ctypes.POINTER(lb_latent_cache), vp, f32, vp, vp, sz, vp]
+    lib.lb_latent_attention.argtypes = [vp, i32, i64, i64, i64, i64, i64, i64, i64, vp, i32, vp, vp, f32, vp, vp, sz, vp]
     lib.lb_attention_forward.restype = i32
-    lib.lb_attention_forward.argtypes = [ctypes.POINTER(lb_attention), vp, vp, vp]
+    lib.lb_attention_forward.argtypes = [vp, vp, vp, vp]
     lib.lb_attention_backward_workspace_bytes.restype = sz
     lib.lb_attention_backward_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
     lib.lb_attention_backward.restype = i32
-    lib.lb_attention_backward.argtypes = [ctypes.POINTER(lb_attention), vp, vp, vp, ctypes.POINTER(lb_attention_grads),
-                                          vp, sz, vp]
+    lib.lb_attention_backward.argtypes = [vp, vp, vp, vp, vp, vp, sz, vp]
     if lib.lb_abi_version() != ABI_VERSION:
         raise RuntimeError("liblittlebit.so ABI version mismatch")
     _lib = lib
@@ -552,43 +552,55 @@ def lb_linear_backward(x, dy, paths: Sequence[LittleBitPath], train: Sequence[Li
 # ----------------------------------------------------------------------------
 # paged latent cache and attention
 # ----------------------------------------------------------------------------
-def _one_device(*tensors):
+# The C structures as packed bytes (native sizes and alignment).
+_PACK_CACHE = struct.Struct("@PiqqqqPqqPP").pack
+_PACK_PATHS = struct.Struct("@10P").pack
+_PACK_ATTN = struct.Struct("@PPPPi14qPPqif").pack
+_PACK_GRADS = struct.Struct("@4P4q").pack
+
+
+def _current_device() -> int:
+    return _torch()._C._cuda_getDevice()
+
+
+def _on_gpu(*tensors):
     """Every tensor on the current GPU (a launch goes to the current device's stream)."""
-    torch = _torch()
-    cur = torch.cuda.current_device()
+    cur = None
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != cur):
+        if t is None:
+            continue
+        d = t.get_device()
+        if d < 0:
+            raise ValueError(f"expected a GPU tensor, got one on {t.device}")
+        if cur is None:
+            cur = _current_device()
+        if d != cur:
             raise ValueError(f"every tensor must be on the current GPU (cuda:{cur}), got one on {t.device}")
 
 
-def _int32(t, shape, name: str) -> int:
-    torch = _torch()
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be int32 of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return _dev_ptr(t, name)
+def _need(t, shape, dtype, name: str):
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _whole(t, shape, dtype, name: str) -> int:
+    """The address of a contiguous tensor of this shape and type."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        _need(t, shape, dtype, name)
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def _freqs(t, d: int) -> int:
-    torch = _torch()
-    if t is None:
-        return 0
-    if t.dtype != torch.float32 or tuple(t.shape) != (d // 2,):
-        raise ValueError(f"freqs must be float32 of shape ({d // 2},), got {t.dtype} {tuple(t.shape)}")
-    return _dev_ptr(t, "freqs")
+    return 0 if t is None else _whole(t, (d // 2,), _T.float32, "freqs")
 
 
-def _rows(t, name: str, dims: int = 3):
-    """(pointer, strides) of a tensor whose last dimension is contiguous."""
-    if t.dim() != dims:
-        raise ValueError(f"{name} must have {dims} dimensions")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+def _rows(t, name: str):
+    """(address, strides) of a tensor whose last dimension is contiguous."""
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name} must be contiguous in its last dimension")
-    return t.data_ptr() if t.numel() else 0, t.stride()[:-1]
-
-
-def _shape(t, shape, dtype, name: str):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr(), st
 
 
 def lb_rotate(x, positions, freqs, inverse: bool = False, out=None, stream=None):
@@ -596,16 +608,22 @@ def lb_rotate(x, positions, freqs, inverse: bool = False, out=None, stream=None)
     (i, i + d / 2); inverse=True turns back, which is also the gradient's map.  x and out may be strided
     (last dimension contiguous), out may be x; returns out."""
     torch = _torch()
+    if x.dim() != 3:
+        raise ValueError("x must be [T, H, d]")
+    shape = x.shape
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _shape(out, x.shape, x.dtype, "out")
-    _one_device(x, positions, freqs, out)
-    T, H, d = x.shape
-    px, (x_t, x_h) = _rows(x, "x")
-    py, (y_t, y_h) = _rows(out, "out")
-    st = load_library().lb_rotate(px, _dtype_code(x), T, H, d, x_t, x_h, _int32(positions, (T,), "positions"),
-                                  _freqs(freqs, d), int(inverse), py, y_t, y_h, _stream(stream))
-    _check(st, "lb_rotate")
+        out = x.new_empty(shape)
+    else:
+        _need(out, shape, x.dtype, "out")
+    _on_gpu(x, positions, freqs, out)
+    T, H, d = shape
+    px, sx = _rows(x, "x")
+    py, sy = _rows(out, "out")
+    st = load_library().lb_rotate(px, _dtype_code(x), T, H, d, sx[0], sx[1], _whole(positions, (T,), torch.int32, "positions"),
+                                  _whole(freqs, (d // 2,), torch.float32, "freqs"), 1 if inverse else 0, py, sy[0], sy[1],
+                                  _stream(stream))
+    if st:
+        _check(st, "lb_rotate")
     return out
 
 
@@ -627,34 +645,37 @@ class LatentCache:
         return cls(torch.empty((n_pages, page_size, lb_latent_row(r, d_rope)), dtype=dtype or torch.bfloat16,
                                device=device), r, d_rope)
 
-    def _struct(self, table, lens, cu):
+    def _packed(self, table, lens, cu) -> bytes:
         d = self.data
-        if d.dim() != 3 or d.shape[2] != lb_latent_row(self.r, self.d_rope) or d.shape[2] == 0:
-            raise ValueError("a cache's data must be [n_pages, page_size, lb_latent_row(r, d_rope)]")
+        row = (2 * self.r + self.d_rope + 31) // 32 * 32
+        if d.dim() != 3 or d.shape[2] != row or not d.is_contiguous():
+            raise ValueError("a cache's data must be contiguous [n_pages, page_size, lb_latent_row(r, d_rope)]")
         if table.dim() != 2:
             raise ValueError("table must be [sequences, pages]")
         B, M = table.shape
-        return lb_latent_cache(_dev_ptr(d, "data"), _dtype_code(d), d.shape[0], d.shape[1], self.r, self.d_rope,
-                               _int32(table, (B, M), "table"), B, M, _int32(lens, (B,), "lens"),
-                               _int32(cu, (B + 1,), "cu"))
+        i32 = _T.int32
+        return _PACK_CACHE(d.data_ptr(), _dtype_code(d), d.shape[0], d.shape[1], self.r, self.d_rope,
+                           _whole(table, (B, M), i32, "table"), B, M, _whole(lens, (B,), i32, "lens"),
+                           _whole(cu, (B + 1,), i32, "cu"))
 
 
 def lb_latent_append(cache: LatentCache, w, k_rope, freqs, table, lens, cu, stream=None):
     """Append latents w [T, 2, r] and rotary keys k_rope [T, d_rope] (None if d_rope is 0; turned by their
     positions with freqs, or stored as they are if it is None): sequence b's tokens are rows cu[b] ..
     cu[b + 1] - 1 and become its last positions below lens[b], on the pages table[b] names."""
-    _one_device(cache.data, w, k_rope, freqs, table, lens, cu)
+    _torch()
+    d = cache.d_rope
+    _on_gpu(cache.data, w, k_rope if d else None, freqs, table, lens, cu)
     T = w.shape[0]
-    if tuple(w.shape) != (T, 2, cache.r):
-        raise ValueError(f"w must be [T, 2, {cache.r}]")
+    pw = _whole(w, (T, 2, cache.r), w.dtype, "w")
     kp, kt = 0, 0
-    if cache.d_rope:
-        _shape(k_rope, (T, cache.d_rope), w.dtype, "k_rope")
-        kp, (kt,) = _rows(k_rope, "k_rope", 2)
-    c = cache._struct(table, lens, cu)
-    st = load_library().lb_latent_append(ctypes.byref(c), _dev_ptr(w, "w"), kp, kt, _dtype_code(w), T,
-                                         _freqs(freqs, cache.d_rope), _stream(stream))
-    _check(st, "lb_latent_append")
+    if d:
+        _need(k_rope, (T, d), w.dtype, "k_rope")
+        kp, (kt, _) = _rows(k_rope, "k_rope")
+    st = load_library().lb_latent_append(cache._packed(table, lens, cu), pw, kp, kt, _dtype_code(w), T,
+                                         _freqs(freqs, d), _stream(stream))
+    if st:
+        _check(st, "lb_latent_append")
 
 
 def lb_latent_attention_workspace_bytes(T: int, n_seq: int, H: int, r: int, d_rope: int) -> int:
@@ -668,57 +689,72 @@ def lb_latent_attention(q, cache: LatentCache, paths: Sequence[LittleBitPath], H
     the fused layer, d_out = Hk (d_nope + d_v), keys first.  q's last d_rope values are turned by their
     positions with freqs (None: taken as they are).  scale defaults to (d_nope + d_rope) ** -0.5; returns
     out [T, H, d_v]."""
-    torch = _torch()
-    _one_device(q, cache.data, freqs, table, lens, cu, out, workspace, *(t for p in paths for t in (p.U, p.h)))
+    _torch()
+    if len(paths) != 2:
+        raise ValueError("exactly two paths (primary, residual) are required")
+    if q.dim() != 3:
+        raise ValueError("q must be [T, H, d_nope + d_rope]")
+    a, b = paths
+    _on_gpu(q, cache.data, freqs, table, lens, cu, out, workspace, a.U, a.h, b.U, b.h)
     T, H, dq = q.shape
-    dn = dq - cache.d_rope
+    r, dr = cache.r, cache.d_rope
+    dn = dq - dr
     if dn < 0:
         raise ValueError("q's heads are narrower than the rotary key")
-    arr, sc = _paths_struct([LittleBitPath(p.U, None, p.h, None, None) for p in paths])
     n_out = Hk * (dn + d_v)
-    for p in paths:
-        if p.h.numel() != n_out or p.U.numel() * p.U.element_size() < lb_packed_bytes(LB_ROLE_U, n_out, cache.r):
-            raise ValueError(f"paths must be those of a layer with d_out = Hk (d_nope + d_v) = {n_out}, r = {cache.r}")
+    nb, w = r // 32, r % 32
+    need = n_out * (4 * nb + (0 if w == 0 else 2 if w <= 16 else 4))
+    for U in (a.U, b.U):
+        if U.numel() * U.element_size() < need or not U.is_contiguous():
+            raise ValueError(f"U must hold the packed signs of d_out = Hk (d_nope + d_v) = {n_out} rows at r = {r}")
+    sdt = a.h.dtype
+    arr = _PACK_PATHS(a.U.data_ptr(), 0, _whole(a.h, (n_out,), sdt, "h"), 0, 0,
+                      b.U.data_ptr(), 0, _whole(b.h, (n_out,), sdt, "h"), 0, 0)
     if out is None:
-        out = torch.empty((T, H, d_v), dtype=q.dtype, device=q.device)
-    _shape(out, (T, H, d_v), q.dtype, "out")
+        out = q.new_empty((T, H, d_v))
     if workspace is None:
-        workspace = _scratch(lb_latent_attention_workspace_bytes(T, lens.shape[0], H, cache.r, cache.d_rope), q.device)
-    pq, (q_t, q_h) = _rows(q, "q")
-    c = cache._struct(table, lens, cu)
+        workspace = _scratch(lb_latent_attention_workspace_bytes(T, lens.shape[0], H, r, dr), q.device)
+    pq, sq = _rows(q, "q")
     st = load_library().lb_latent_attention(
-        pq, _dtype_code(q), T, H, Hk, dn, d_v, q_t, q_h, arr, sc, ctypes.byref(c), _freqs(freqs, cache.d_rope),
-        float(dq ** -0.5 if scale is None else scale), _dev_ptr(out, "out"), _dev_ptr(workspace, "workspace"),
-        workspace.numel() * workspace.element_size(), _stream(stream))
-    _check(st, "lb_latent_attention")
+        pq, _dtype_code(q), T, H, Hk, dn, d_v, sq[0], sq[1], arr, _dtype_code(a.h), cache._packed(table, lens, cu),
+        _freqs(freqs, dr), dq ** -0.5 if scale is None else scale, _whole(out, (T, H, d_v), q.dtype, "out"),
+        _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream))
+    if st:
+        _check(st, "lb_latent_attention")
     return out
 
 
-def _attention_struct(q, k, v, k_rope, cu_q, cu_k, causal, scale):
+def _packed_attention(q, k, v, k_rope, cu_q, cu_k, causal, scale):
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise ValueError("q, k and v must be [tokens, heads, width]")
+    dt = q.dtype
     Tq, H, dq = q.shape
     Tk, Hk, dn = k.shape
-    d_v = v.shape[-1]
-    dr = 0 if k_rope is None else k_rope.shape[-1]
+    d_v = v.shape[2]
+    dr, pr, kr_t = 0, 0, 0
+    if k_rope is not None:
+        dr = k_rope.shape[-1]
+        _need(k_rope, (Tk, dr), dt, "k_rope")
+        pr, (kr_t, _) = _rows(k_rope, "k_rope")
     if dn + dr != dq:
         raise ValueError("q's heads must be as wide as k's and k_rope's together")
-    _shape(k, (Tk, Hk, dn), q.dtype, "k")
-    _shape(v, (Tk, Hk, d_v), q.dtype, "v")
-    pq, (q_t, q_h) = _rows(q, "q")
-    pk, (k_t, k_h) = _rows(k, "k")
-    pv, (v_t, v_h) = _rows(v, "v")
-    pr, kr_t = 0, 0
-    if dr:
-        _shape(k_rope, (Tk, dr), q.dtype, "k_rope")
-        pr, (kr_t,) = _rows(k_rope, "k_rope", 2)
+    _need(k, (Tk, Hk, dn), dt, "k")
+    _need(v, (Tk, Hk, d_v), dt, "v")
+    pq, sq = _rows(q, "q")
+    pk, sk = _rows(k, "k")
+    pv, sv = _rows(v, "v")
     if (cu_q is None) != (cu_k is None):
         raise ValueError("cu_q and cu_k are given together")
-    n = 0 if cu_q is None else cu_q.shape[0] - 1
-    if cu_q is not None and n < 0:
-        raise ValueError("cu_q must hold at least one value")
-    return lb_attention(pq, pk, pv, pr, _dtype_code(q), Tq, Tk, H, Hk, dn, dr, d_v, q_t, q_h, k_t, k_h, v_t, v_h, kr_t,
-                        0 if cu_q is None else _int32(cu_q, (n + 1,), "cu_q"),
-                        0 if cu_k is None else _int32(cu_k, (n + 1,), "cu_k"), n, int(causal),
-                        float(dq ** -0.5 if scale is None else scale)), (Tq, Tk, H, Hk, dn, dr, d_v)
+    n, pcq, pck = 0, 0, 0
+    if cu_q is not None:
+        if cu_q.dim() != 1 or cu_q.shape[0] < 1:
+            raise ValueError("cu_q must hold the sequences' prefix sums")
+        n = cu_q.shape[0] - 1
+        pcq = _whole(cu_q, (n + 1,), _T.int32, "cu_q")
+        pck = _whole(cu_k, (n + 1,), _T.int32, "cu_k")
+    return _PACK_ATTN(pq, pk, pv, pr, _dtype_code(q), Tq, Tk, H, Hk, dn, dr, d_v, sq[0], sq[1], sk[0], sk[1], sv[0], sv[1],
+                      kr_t, pcq, pck, n, 1 if causal else 0, dq ** -0.5 if scale is None else scale), (
+                          Tq, Tk, H, Hk, dn, dr, d_v)
 
 
 def lb_attention_forward(q, k, v, k_rope=None, cu_q=None, cu_k=None, causal: bool = True, scale=None, o=None, lse=None,
@@ -728,16 +764,16 @@ def lb_attention_forward(q, k, v, k_rope=None, cu_q=None, cu_k=None, causal: boo
     dimension; cu_q, cu_k int32 prefix sums of packed sequences (None: one sequence).  scale defaults to
     (d_nope + d_rope) ** -0.5.  Returns (o [Tq, H, d_v], lse [Tq, H] fp32)."""
     torch = _torch()
-    _one_device(q, k, v, k_rope, cu_q, cu_k, o, lse)
-    a, (Tq, _, H, _, _, _, d_v) = _attention_struct(q, k, v, k_rope, cu_q, cu_k, causal, scale)
+    _on_gpu(q, k, v, k_rope, cu_q, cu_k, o, lse)
+    a, (Tq, _, H, _, _, _, d_v) = _packed_attention(q, k, v, k_rope, cu_q, cu_k, causal, scale)
     if o is None:
-        o = torch.empty((Tq, H, d_v), dtype=q.dtype, device=q.device)
+        o = q.new_empty((Tq, H, d_v))
     if lse is None:
-        lse = torch.empty((Tq, H), dtype=torch.float32, device=q.device)
-    _shape(o, (Tq, H, d_v), q.dtype, "o")
-    _shape(lse, (Tq, H), torch.float32, "lse")
-    st = load_library().lb_attention_forward(ctypes.byref(a), _dev_ptr(o, "o"), _dev_ptr(lse, "lse"), _stream(stream))
-    _check(st, "lb_attention_forward")
+        lse = q.new_empty((Tq, H), dtype=torch.float32)
+    st = load_library().lb_attention_forward(a, _whole(o, (Tq, H, d_v), q.dtype, "o"),
+                                             _whole(lse, (Tq, H), torch.float32, "lse"), _stream(stream))
+    if st:
+        _check(st, "lb_attention_forward")
     return o, lse
 
 
@@ -750,29 +786,33 @@ def lb_attention_backward(q, k, v, k_rope, o, lse, d_o, cu_q=None, cu_k=None, ca
     """Gradients of lb_attention_forward for d_o [Tq, H, d_v] (contiguous); dk and dv may be strided views (the
     two parts of the fused layer's dy).  Returns (dq, dk, dv, dk_rope) (dk_rope None without a rotary key)."""
     torch = _torch()
-    _one_device(q, k, v, k_rope, o, lse, d_o, cu_q, cu_k, dq, dk, dv, dk_rope, workspace)
-    a, (Tq, Tk, H, Hk, dn, dr, d_v) = _attention_struct(q, k, v, k_rope, cu_q, cu_k, causal, scale)
-    new = dict(dtype=q.dtype, device=q.device)
-    dq = torch.empty((Tq, H, dn + dr), **new) if dq is None else dq
-    dk = torch.empty((Tk, Hk, dn), **new) if dk is None else dk
-    dv = torch.empty((Tk, Hk, d_v), **new) if dv is None else dv
-    if dr and dk_rope is None:
-        dk_rope = torch.empty((Tk, dr), **new)
-    for t, shape, name in ((o, (Tq, H, d_v), "o"), (d_o, (Tq, H, d_v), "d_o"), (dq, (Tq, H, dn + dr), "dq"),
-                           (dk, (Tk, Hk, dn), "dk"), (dv, (Tk, Hk, d_v), "dv")):
-        _shape(t, shape, q.dtype, name)
-    _shape(lse, (Tq, H), torch.float32, "lse")
+    _on_gpu(q, k, v, k_rope, o, lse, d_o, cu_q, cu_k, dq, dk, dv, dk_rope, workspace)
+    a, (Tq, Tk, H, Hk, dn, dr, d_v) = _packed_attention(q, k, v, k_rope, cu_q, cu_k, causal, scale)
+    dt = q.dtype
+    dq = q.new_empty((Tq, H, dn + dr)) if dq is None else dq
+    if dk is None:
+        dk = q.new_empty((Tk, Hk, dn))
+    else:
+        _need(dk, (Tk, Hk, dn), dt, "dk")
+    if dv is None:
+        dv = q.new_empty((Tk, Hk, d_v))
+    else:
+        _need(dv, (Tk, Hk, d_v), dt, "dv")
+    pr = 0
     if dr:
-        _shape(dk_rope, (Tk, dr), q.dtype, "dk_rope")
-    pk, (dk_t, dk_h) = _rows(dk, "dk")
-    pv, (dv_t, dv_h) = _rows(dv, "dv")
-    g = lb_attention_grads(_dev_ptr(dq, "dq"), pk, pv, _dev_ptr(dk_rope, "dk_rope") if dr else 0, dk_t, dk_h, dv_t, dv_h)
+        dk_rope = q.new_empty((Tk, dr)) if dk_rope is None else dk_rope
+        pr = _whole(dk_rope, (Tk, dr), dt, "dk_rope")
+    pk, sk = _rows(dk, "dk")
+    pv, sv = _rows(dv, "dv")
+    g = _PACK_GRADS(_whole(dq, (Tq, H, dn + dr), dt, "dq"), pk, pv, pr, sk[0], sk[1], sv[0], sv[1])
     if workspace is None:
         workspace = _scratch(lb_attention_backward_workspace_bytes(Tq, Tk, H, Hk, dr), q.device)
     st = load_library().lb_attention_backward(
-        ctypes.byref(a), _dev_ptr(o, "o"), _dev_ptr(lse, "lse"), _dev_ptr(d_o, "d_o"), ctypes.byref(g),
-        _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream))
-    _check(st, "lb_attention_backward")
+        a, _whole(o, (Tq, H, d_v), dt, "o"), _whole(lse, (Tq, H), torch.float32, "lse"),
+        _whole(d_o, (Tq, H, d_v), dt, "d_o"), g, _dev_ptr(workspace, "workspace"),
+        workspace.numel() * workspace.element_size(), _stream(stream))
+    if st:
+        _check(st, "lb_attention_backward")
     return dq, dk, dv, dk_rope if dr else None
 
 

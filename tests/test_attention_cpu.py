@@ -203,3 +203,15 @@ def test_binding_refuses_cpu_tensors_and_wrong_shapes(lib):
                 (x[0], pos, f)):
         with pytest.raises(ValueError):
             lb.lb_rotate(*bad)
+
+
+def test_packed_structures_match_the_header(lib):
+    import struct
+    for pack, cls, n in (("@PiqqqqPqqPP", lb.lb_latent_cache, 11), ("@PPPPi14qPPqif", lb.lb_attention, 24),
+                         ("@4P4q", lb.lb_attention_grads, 8), ("@10P", lb.lb_path * 2, 10)):
+        vals = list(range(1, n + 1))
+        raw = struct.pack(pack, *vals)
+        assert len(raw) == ctypes.sizeof(cls)
+        if hasattr(cls, "_fields_"):
+            got = cls.from_buffer_copy(raw)
+            assert [getattr(got, f) for f, _ in cls._fields_] == vals
