@@ -17,8 +17,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBM = 128;  // query rows of a workgroup (4 waves x 32)
 constexpr int kBN = 64;   // keys of a step
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 
 struct FwdArgs {
   AttnArgs a;
@@ -126,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd(FwdArgs f) {
     tm = fmaxf(tm, __shfl_xor(tm, 32));
     if (__any(tm > mx)) {
       const float m2 = fmaxf(mx, tm);
-      const float r = m2 == -INFINITY ? 1.0f : exp2f((mx - m2) * sc);
+      const float r = m2 == -INFINITY ? 1.0f : exp2_fast((mx - m2) * sc);
       mx = m2;
       sum *= r;
 #pragma unroll
@@ -139,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd(FwdArgs f) {
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        s[b][e] = exp2f(s[b][e] * sc - mz);
+        s[b][e] = exp2_fast(s[b][e] * sc - mz);
         sum += s[b][e];
       }
 #pragma unroll

@@ -17,7 +17,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBM = 128;  // rows a workgroup owns
-constexpr float kLog2e = 1.4426950408889634f;
 
 struct BwdArgs {
   AttnArgs a;
@@ -184,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
         const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          float p = exp2f(s[e + q] * sc - lv[q]);
+          float p = exp2_fast(s[e + q] * sc - lv[q]);
           if (mask && i0 + row + q + off < j) p = 0.0f;
           s[e + q] = p;
           dp[e + q] = p == 0.0f ? 0.0f : p * (dp[e + q] - dl[q]) * fac;
@@ -323,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_queries(BwdArgs f) {
       const bool mask = j0 + 32 * b + 31 > lim_lo;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        float p = exp2f(s[e] * sc - l2);
+        float p = exp2_fast(s[e] * sc - l2);
         if (mask && j0 + 32 * b + 8 * (e >> 2) + 4 * hh + (e & 3) > lim) p = 0.0f;
         dp[e] = p == 0.0f ? 0.0f : p * (dp[e] - del) * fac;
       }

@@ -25,7 +25,6 @@ namespace {
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef __attribute__((address_space(1))) const void* glb_ptr;
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr size_t kLdsMax = 163840;
 constexpr int kCols = 32;  // query rows of an item (columns of the tiles)
 constexpr int kG = 256;    // workgroups of split (one a CU)
@@ -57,7 +56,7 @@ __host__ LatPlan lat_plan(int r, int d_rope, int es) {
   // a wave's registers hold 12 units (q' and the sums); wider rows go to four waves
   p.ncw = p.nu <= 12 ? 1 : 4;
   p.nuw = (p.nu + p.ncw - 1) / p.ncw;
-  p.upw = p.nuw <= 4 ? 4 : (p.nuw + 1) / 2 * 2;
+  p.upw = p.nuw <= 4 ? 4 : p.ncw == 1 ? p.nuw : (p.nuw + 1) / 2 * 2;
   p.tpt = 32;
   p.tile_bytes = p.nuw * 32 * 32 * es;
   if (p.ncw == 1) {
@@ -448,29 +447,28 @@ template <int CD>
 __device__ __forceinline__ int swz(int t) {
   return CD == kDtF32 ? (t >> 1) & 7 : (t >> 2) & 3;
 }
-// row t (of tpt) at columns 16 chunk + 8 (lane / 32) ..
+// row lane % tpt of a unit at columns 16 half + 8 (lane / 32) ..
 template <int CD>
-__device__ __forceinline__ Frag<CD> tile_rows(const char* tile, int tpt, int chunk, int lane) {
+__device__ __forceinline__ Frag<CD> tile_rows(const char* unit, int tpt, int half, int lane) {
   constexpr int PU = 2 * esize<CD>();
   const int t = lane & (tpt - 1), s = swz<CD>(t);
-  const char* p = tile + ((chunk >> 1) * tpt + t) * PU * 16;
+  const char* p = unit + t * PU * 16;
   Frag<CD> f;
   if constexpr (CD == kDtF32) {
-    const int q = 4 * (chunk & 1) + 2 * (lane >> 5);
+    const int q = 4 * half + 2 * (lane >> 5);
     f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * (q ^ s));
     f.v[1] = *reinterpret_cast<const u32x4*>(p + 16 * ((q + 1) ^ s));
   } else {
-    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * ((2 * (chunk & 1) + (lane >> 5)) ^ s));
+    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * ((2 * half + (lane >> 5)) ^ s));
   }
   return f;
 }
-// columns 32 u + lane % 32 at the 16 tokens of slice s (slots as in attn_common.h)
+// columns lane % 32 of a unit at the 16 tokens of slice s (slots as in attn_common.h)
 template <int CD>
-__device__ __forceinline__ Frag<CD> tile_cols(const char* tile, int tpt, int s, int u, int lane) {
+__device__ __forceinline__ Frag<CD> tile_cols(const char* t, int s, int lane) {
   constexpr int PU = 2 * esize<CD>();
   Frag<CD> f;
   const int hh = lane >> 5;
-  const char* t = tile + u * tpt * PU * 16;
   if constexpr (CD == kDtF32) {
     const int q = (lane & 31) >> 2;
 #pragma unroll
@@ -508,6 +506,8 @@ template <int CD, int TQ, int TP, int UPW, bool CSPLIT>
 __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   constexpr int ES = esize<CD>(), PU = 2 * ES;
+  // every wave holds UPW units (else up to UPW: absent ones meet a zero q' at the last one's place)
+  constexpr bool EXACT = !CSPLIT && UPW > 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, ml_ = lane & 31;
   const CacheArgs& c = a.c;
@@ -522,12 +522,12 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
   int x = x_begin;
   const int tw = CSPLIT ? 0 : wave, cw = CSPLIT ? wave : 0;
   const int u0 = cw * p.nuw;                                       // the wave's units of the row
-  const int nu = max(0, min(p.nuw, p.nu - u0)), vu = max(0, min(nu, p.vu - u0));
+  const int nu = EXACT ? UPW : min(p.nuw, p.nu - u0), vu = max(0, min(nu, p.vu - u0));
   char* tiles = smem + wave * p.stages * p.tile_bytes;
   float* xchg = reinterpret_cast<float*>(smem + (CSPLIT ? 4 : p.ntw) * p.stages * p.tile_bytes);
   const int64_t row_bytes = static_cast<int64_t>(c.row) * esize<CD>();
   const char* data = static_cast<const char*>(c.data) + u0 * 32 * esize<CD>();
-  const int ow = p.vu * 32;
+  const int ow = p.vu * 32, unit_bytes = p.tpt * PU * 16;
 
   while (x < x_end) {
     SeqWork sw;
@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
       }
 #pragma unroll
       for (int u = 0; u < UPW; ++u) {
-        if (u < nu) {
+        if (EXACT || u < nu) {
 #pragma unroll
           for (int n = 0; n < NL; ++n) {
             if (n * TPL < p.tpt)
@@ -604,15 +604,44 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
     const rsrc_t qr = make_rsrc_uniform(qbase, kCols * TQ * static_cast<uint32_t>(row_bytes));
     const uint32_t qo = rr * TQ * static_cast<uint32_t>(row_bytes) + 8 * hh * ES;
     Frag<CD> qf[2 * UPW][TQ];
+    constexpr int FP = ES / 2;  // 16-byte pieces of a fragment a lane
+    if (!CSPLIT && p.stages == 2 && p.ntw >= TQ) {
+      // the token waves need the same fragments: each loads a part of them into the second
+      // tiles (term n into wave n's), and all read them from there
+      const int nf = 2 * nu * FP;
+      for (int i = wave; i < TQ * nf; i += p.ntw) {
+        const int n = i / nf, k = i - n * nf;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, (lds_ptr)(smem + (2 * n + 1) * p.tile_bytes + 1024 * k), 16,
+                                                 qo + (k / FP) * 16 * ES + (k % FP) * 16,
+                                                 n * static_cast<uint32_t>(row_bytes), 0, 0);
+      }
+      wait_loads();
+      lds_barrier();
 #pragma unroll
-    for (int k = 0; k < 2 * UPW; ++k) {
+      for (int k = 0; k < 2 * UPW; ++k) {
 #pragma unroll
-      for (int n = 0; n < TQ; ++n) {
-        qf[k][n] = frag_zero<CD>();
-        if (k < 2 * nu) {
-          const uint32_t so = n * static_cast<uint32_t>(row_bytes);
-          qf[k][n].v[0] = __builtin_amdgcn_raw_buffer_load_b128(qr, qo + 16 * k * ES, so, 0);
-          if constexpr (CD == kDtF32) qf[k][n].v[1] = __builtin_amdgcn_raw_buffer_load_b128(qr, qo + 16 * k * ES + 16, so, 0);
+        for (int n = 0; n < TQ; ++n) {
+          qf[k][n] = frag_zero<CD>();
+          if (EXACT || k < 2 * nu) {
+            const char* src = smem + (2 * n + 1) * p.tile_bytes + 1024 * FP * k + 16 * lane;
+            qf[k][n].v[0] = *reinterpret_cast<const u32x4*>(src);
+            if constexpr (CD == kDtF32) qf[k][n].v[1] = *reinterpret_cast<const u32x4*>(src + 1024);
+          }
+        }
+      }
+      lds_barrier();
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2 * UPW; ++k) {
+#pragma unroll
+        for (int n = 0; n < TQ; ++n) {
+          qf[k][n] = frag_zero<CD>();
+          if (EXACT || k < 2 * nu) {
+            const uint32_t so = n * static_cast<uint32_t>(row_bytes);
+            qf[k][n].v[0] = __builtin_amdgcn_raw_buffer_load_b128(qr, qo + 16 * k * ES, so, 0);
+            if constexpr (CD == kDtF32)
+              qf[k][n].v[1] = __builtin_amdgcn_raw_buffer_load_b128(qr, qo + 16 * k * ES + 16, so, 0);
+          }
         }
       }
     }
@@ -642,11 +671,13 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
 #pragma unroll
-      for (int k = 0; k < 2 * UPW; ++k) {
-        if (k < 2 * nu) {
-          const Frag<CD> kf = tile_rows<CD>(tile, p.tpt, k, lane);
+      for (int u = 0; u < UPW; ++u) {
+        const char* unit = tile + (EXACT ? u : min(u, nu - 1)) * unit_bytes;
 #pragma unroll
-          for (int n = 0; n < TQ; ++n) acc = mma32<CD>(kf, qf[k][n], acc);
+        for (int k = 0; k < 2; ++k) {
+          const Frag<CD> kf = tile_rows<CD>(unit, p.tpt, k, lane);
+#pragma unroll
+          for (int n = 0; n < TQ; ++n) acc = mma32<CD>(kf, qf[2 * u + k][n], acc);
         }
       }
       if constexpr (CSPLIT) {
@@ -682,23 +713,23 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 #pragma unroll
       for (int e = 1; e < 16; ++e) tm = fmaxf(tm, acc[e]);
       tm = fmaxf(tm, __shfl_xor(tm, 32));
-      if (__any(tm > mx)) {
+      // sums are kept relative to mx, a maximum that follows once it is 2^kSlack behind: a
+      // probability is then at most 2^kSlack, which neither type nor sum minds
+      if (__any(tm > mx + kSlack)) {
         const float m2 = fmaxf(mx, tm);
-        const float f = m2 == -INFINITY ? 1.0f : exp2f(mx - m2);
+        const float f = m2 == -INFINITY ? 1.0f : exp2_fast(mx - m2);
         mx = m2;
         sum *= f;
 #pragma unroll
         for (int u = 0; u < UPW; ++u) {
-          if (u < vu) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[u][e] *= f;
-          }
+          for (int e = 0; e < 16; ++e) o[u][e] *= f;
         }
       }
       const float mz = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        acc[e] = exp2f(acc[e] - mz);
+        acc[e] = exp2_fast(acc[e] - mz);
         sum += acc[e];
       }
 #pragma unroll
@@ -711,13 +742,12 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) pv[e] = acc[8 * sl + e];
         to_terms<CD, TP>(pv, pf);
+        // (the rotary units too: their sums are not read)
 #pragma unroll
         for (int u = 0; u < UPW; ++u) {
-          if (u < vu) {
-            const Frag<CD> vf = tile_cols<CD>(tile, p.tpt, sl, u, lane);
+          const Frag<CD> vf = tile_cols<CD>(tile + (EXACT ? u : min(u, nu - 1)) * unit_bytes, sl, lane);
 #pragma unroll
-            for (int n = 0; n < TP; ++n) o[u] = mma32<CD>(vf, pf[n], o[u]);
-          }
+          for (int n = 0; n < TP; ++n) o[u] = mma32<CD>(vf, pf[n], o[u]);
         }
       }
       if (p.stages == 2) okm = okn;
@@ -765,7 +795,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
       }
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        f[w] = f[w] == -INFINITY ? 0.0f : exp2f(f[w] - top);
+        f[w] = f[w] == -INFINITY ? 0.0f : exp2_fast(f[w] - top);
         if (w < p.ntw) l += f[w] * rml[(w * kCols + m) * 2 + 1];
       }
       if (cq0 == 0) *reinterpret_cast<float2*>(pm + 2 * m) = make_float2(top, l);
@@ -846,7 +876,7 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
   float l = 0.0f;
   for (int i = lane; i < n; i += 64) {
     const float* q = j.ml + ((slot0 + i) * kCols + m) * 2;
-    const float f = top == -INFINITY ? 0.0f : exp2f(q[0] - top);
+    const float f = top == -INFINITY ? 0.0f : exp2_fast(q[0] - top);
     l += f * q[1];
     if (tid < 64) wt[i] = f;
   }
@@ -906,9 +936,13 @@ hipError_t split_cd(const SplitArgs& s, hipStream_t stream) {
   if (s.p.ncw == 1) {
     switch (s.p.upw) {
       case 4: return split_launch<CD, TQ, TP, 4, false>(s, stream);
+      case 5: return split_launch<CD, TQ, TP, 5, false>(s, stream);
       case 6: return split_launch<CD, TQ, TP, 6, false>(s, stream);
+      case 7: return split_launch<CD, TQ, TP, 7, false>(s, stream);
       case 8: return split_launch<CD, TQ, TP, 8, false>(s, stream);
+      case 9: return split_launch<CD, TQ, TP, 9, false>(s, stream);
       case 10: return split_launch<CD, TQ, TP, 10, false>(s, stream);
+      case 11: return split_launch<CD, TQ, TP, 11, false>(s, stream);
       default: return split_launch<CD, TQ, TP, 12, false>(s, stream);
     }
   }
