@@ -26,7 +26,7 @@ SOURCES = ["api.cpp", "pack.hip", "decode.hip", "decode_mma.hip", "prefill.hip",
 _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 EXTRA_FLAGS = {"decode.hip": ["-ffp-contract=off"], "stream.hip": ["-ffp-contract=off"],
                "stream_mma.hip": _VGPR_MFMA, "decode_mma.hip": _VGPR_MFMA, "backward.hip": _VGPR_MFMA,
-               "latent_attn.hip": _VGPR_MFMA, "attention.hip": _VGPR_MFMA, "attention_bwd.hip": _VGPR_MFMA}
+               "latent_attn.hip": _VGPR_MFMA, "attention_bwd.hip": _VGPR_MFMA}
 ARCH = os.environ.get("LB_OFFLOAD_ARCH", "gfx950")
 
 

@@ -16,7 +16,11 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBM = 128;  // query rows of a workgroup (4 waves x 32)
-constexpr int kBN = 64;   // keys of a step
+// keys of a step: two tiles of 192 + 128 columns fill half of a CU's LDS (fp32: all of it)
+template <int DT>
+constexpr int keys_of() {
+  return DT == kDtF32 ? 32 : 64;
+}
 
 struct FwdArgs {
   AttnArgs a;
@@ -25,14 +29,13 @@ struct FwdArgs {
   int n_tiles;  // work items per head (an upper bound)
 };
 
-// the columns [0, 16 KC) of a key row: k, then the shared rotary key
+// KC: 16-wide slices of a key's width, VT: 32-wide tiles of a value's.  Two tiles of K
+// and V: the next one's loads run during the products with this one.
 template <int DT, int KC, int VT>
-__global__ void __launch_bounds__(kThreads, 2) attn_fwd(FwdArgs f) {
-  constexpr int KW = 16 * KC, VW = 32 * VT;
-  constexpr int KS = tile_stride<DT>(KW), VS = tile_stride<DT>(VW);
+__global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_fwd(FwdArgs f) {
+  constexpr int KW = 16 * KC, VW = 32 * VT, BN = keys_of<DT>();
+  constexpr int KB = tile_bytes<DT, BN, KW>(), TB = KB + tile_bytes<DT, BN, VW>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  char* kt = smem;
-  char* vt = smem + kBN * KS;
   const AttnArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, col = lane & 31;
@@ -41,6 +44,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd(FwdArgs f) {
   const int kvh = hi_ % a.Hk, h = kvh * G + hi_ / a.Hk;
   int seq, tile;
   if (!find_tile(a.cu_q, a.n_seq, a.Tq, kBM, id / a.H, lane, seq, tile)) return;
+  seq = __builtin_amdgcn_readfirstlane(seq), tile = __builtin_amdgcn_readfirstlane(tile);
   int q_lo, q_hi, k_lo, k_hi;
   seq_range(a.cu_q, seq, a.Tq, q_lo, q_hi);
   seq_range(a.cu_k, seq, a.Tk, k_lo, k_hi);
@@ -53,8 +57,18 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd(FwdArgs f) {
   const int lim = a.causal ? min(nk - 1, i + off) : nk - 1;  // its last key
   const int lim_lo = a.causal ? min(nk - 1, i0 + 32 * wave + off) : nk - 1;
   const int n_end = a.causal ? min(nk, min(i0 + kBM, nq) + off) : nk;
+  const int w_end = a.causal ? min(n_end, i0 + 32 * wave + 32 + off) : n_end;  // this wave's last key, and one
 
   constexpr int ES = esize<DT>();
+  const char* kp = static_cast<const char*>(a.k) + (k_lo * a.k_t + kvh * a.k_h) * ES;
+  const char* vp = static_cast<const char*>(a.v) + (k_lo * a.v_t + kvh * a.v_h) * ES;
+  const char* rp = static_cast<const char*>(a.k_rope) + k_lo * a.kr_t * ES;
+  auto issue = [&](int j0, char* t) {
+    tile_load<DT, BN, KW, kThreads>(t, kp + j0 * a.k_t * ES, a.k_t, a.d_nope, rp + j0 * a.kr_t * ES, a.kr_t, a.d_rope,
+                                    nk - j0, f.vec, tid);
+    tile_load<DT, BN, VW, kThreads>(t + KB, vp + j0 * a.v_t * ES, a.v_t, dv, nullptr, 0, 0, nk - j0, f.vec, tid);
+  };
+  if (n_end > 0) issue(0, smem);
   const char* qp = static_cast<const char*>(a.q) + ((q_lo + min(i, nq - 1)) * a.q_t + h * a.q_h) * ES;
   Frag<DT> qf[KC];
 #pragma unroll
@@ -68,61 +82,53 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd(FwdArgs f) {
   float mx = -INFINITY, sum = 0.0f;
   const float sc = a.scale * kLog2e;
 
-  constexpr int KL = kBN * KW / 8 / kThreads, VL = kBN * VW / 8 / kThreads;  // groups of eight per thread
-  Frag<DT> kr[KL], vr[VL];
-  const char* kp = static_cast<const char*>(a.k) + kvh * a.k_h * ES;
-  const char* vp = static_cast<const char*>(a.v) + kvh * a.v_h * ES;
-  const char* rp = static_cast<const char*>(a.k_rope);
-  auto fetch = [&](int j0) {
-#pragma unroll
-    for (int n = 0; n < KL; ++n) {
-      const int u = tid + n * kThreads, row = u / (KW / 8), c = 8 * (u % (KW / 8));
-      const int64_t t = k_lo + j0 + row;
-      kr[n] = j0 + row < nk ? load8_joined<DT>(kp + t * a.k_t * ES, a.d_nope, rp + t * a.kr_t * ES, a.d_rope, c, f.vec)
-                            : frag_zero<DT>();
-    }
-#pragma unroll
-    for (int n = 0; n < VL; ++n) {
-      const int u = tid + n * kThreads, row = u / (VW / 8), c = 8 * (u % (VW / 8));
-      vr[n] = j0 + row < nk ? load8<DT>(vp + (k_lo + j0 + row) * a.v_t * ES, c, dv, f.vec) : frag_zero<DT>();
-    }
-  };
-  if (n_end > 0) fetch(0);
-  for (int j0 = 0; j0 < n_end; j0 += kBN) {
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < KL; ++n) {
-      const int u = tid + n * kThreads;
-      tile_put<DT>(kt, KS, u / (KW / 8), 8 * (u % (KW / 8)), kr[n]);
-    }
-#pragma unroll
-    for (int n = 0; n < VL; ++n) {
-      const int u = tid + n * kThreads;
-      tile_put<DT>(vt, VS, u / (VW / 8), 8 * (u % (VW / 8)), vr[n]);
-    }
-    __syncthreads();
-    if (j0 + kBN < n_end) fetch(j0 + kBN);
+  for (int j0 = 0; j0 < n_end; j0 += BN) {
+    char* kt = smem + (j0 / BN & 1) * TB;
+    const char* vt = kt + KB;
+    wait_loads();
+    lds_barrier();  // everyone's loads have arrived, and everyone is done with the other tile
+    if (j0 + BN < n_end) issue(j0 + BN, smem + (~(j0 / BN) & 1) * TB);
+    if (j0 >= w_end) continue;
 
-    floatx16 s[2];
+    // S^T: groups of GK fragments, each read while the one before is multiplied
+    constexpr int GK = DT == kDtF32 ? 1 : KC % 4 == 0 ? 4 : 3, NG = BN / 32 * KC / GK;
+    floatx16 s[BN / 32];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < BN / 32; ++b)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
+    Frag<DT> kf[2][GK];
 #pragma unroll
-      for (int c = 0; c < KC; ++c) s[b] = mma32<DT>(frag_rows<DT>(kt, KS, 32 * b, 16 * c, lane), qf[c], s[b]);
+    for (int g = -1; g < NG; ++g) {
+      if (g + 1 < NG) {
+#pragma unroll
+        for (int n = 0; n < GK; ++n) {
+          const int c = (g + 1) * GK + n;
+          kf[(g + 1) & 1][n] = frag_rows<DT, BN>(kt, 32 * (c / KC), 16 * (c % KC), lane);
+        }
+      }
+      keep_order();
+      if (g >= 0) {
+#pragma unroll
+        for (int n = 0; n < GK; ++n) {
+          const int c = g * GK + n;
+          s[c / KC] = mma32<DT>(kf[g & 1][n], qf[c % KC], s[c / KC]);
+        }
+      }
     }
-    if (j0 + kBN - 1 > lim_lo) {
+    if (j0 + BN - 1 > lim_lo) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < BN / 32; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (j0 + 32 * b + 8 * (e >> 2) + 4 * hh + (e & 3) > lim) s[b][e] = -INFINITY;
     }
     float tm = s[0][0];
 #pragma unroll
-    for (int e = 1; e < 32; ++e) tm = fmaxf(tm, s[e >> 4][e & 15]);
+    for (int e = 1; e < BN / 2; ++e) tm = fmaxf(tm, s[e >> 4][e & 15]);
     tm = fmaxf(tm, __shfl_xor(tm, 32));
-    if (__any(tm > mx)) {
+    // sums are kept relative to mx, a maximum that follows once it is 2^kSlack behind
+    if (__any((tm - mx) * sc > kSlack || (mx == -INFINITY && tm > mx))) {
       const float m2 = fmaxf(mx, tm);
       const float r = m2 == -INFINITY ? 1.0f : exp2_fast((mx - m2) * sc);
       mx = m2;
@@ -133,23 +139,26 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd(FwdArgs f) {
         for (int e = 0; e < 16; ++e) o[t][e] *= r;
     }
     const float mz = mx == -INFINITY ? 0.0f : mx * sc;
+    // O^T: slices of 16 keys
+    Frag<DT> vf[2][VT];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int sl = -1; sl < BN / 16; ++sl) {
+      if (sl + 1 < BN / 16) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[b][e] = exp2_fast(s[b][e] * sc - mz);
-        sum += s[b][e];
+        for (int t = 0; t < VT; ++t) vf[(sl + 1) & 1][t] = frag_cols<DT, BN>(vt, 16 * (sl + 1), 32 * t, lane);
       }
-#pragma unroll
-      for (int sl = 0; sl < 2; ++sl) {
+      keep_order();
+      if (sl >= 0) {
         // the probabilities in the operands' type: one rounding each (their sum keeps 32 bits)
         float pv[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pv[e] = s[b][8 * sl + e];
+        for (int e = 0; e < 8; ++e) {
+          pv[e] = exp2_fast(s[sl >> 1][8 * (sl & 1) + e] * sc - mz);
+          sum += pv[e];
+        }
         const Frag<DT> pf = frag_from<DT>(pv);
 #pragma unroll
-        for (int t = 0; t < VT; ++t)
-          o[t] = mma32<DT>(frag_cols<DT>(vt, VS, 32 * b + 16 * sl, 32 * t, lane), pf, o[t]);
+        for (int t = 0; t < VT; ++t) o[t] = mma32<DT>(vf[sl & 1][t], pf, o[t]);
       }
     }
   }
@@ -170,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd(FwdArgs f) {
 template <int DT, int KC, int VT>
 hipError_t fwd_launch(const FwdArgs& f, hipStream_t stream) {
   static LdsLimit limit;
-  const size_t lds = static_cast<size_t>(kBN) * (tile_stride<DT>(16 * KC) + tile_stride<DT>(32 * VT));
+  constexpr size_t lds = 2 * static_cast<size_t>(tile_bytes<DT, keys_of<DT>(), 16 * KC + 32 * VT>());
   const hipError_t e = raise_lds(reinterpret_cast<const void*>(&attn_fwd<DT, KC, VT>), lds, limit);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((attn_fwd<DT, KC, VT>), dim3(static_cast<uint32_t>(f.n_tiles) * f.a.H), dim3(kThreads), lds, stream,

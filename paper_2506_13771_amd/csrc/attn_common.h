@@ -166,57 +166,147 @@ __device__ __forceinline__ void store4(void* row, int col, int n, bool vec, floa
 }
 
 // ---------------------------------------------------------------------------
-// LDS tiles: rows of W elements, the row stride a number of 16-byte slots that is 3,
-// 5, 11 or 13 modulo 16.  Row-wise reads (16 rows at one slot) then meet 16 different
-// slots of the 64 banks, transposed reads (8 rows of 4 slots) at most 3 in one slot
-// where 2 is the least.
+// LDS tiles of R rows, by units of 32 columns: [unit][row][pieces of 16 bytes], PU pieces
+// a row (4; fp32: 8), piece q of row t at q ^ swz(t).  Row-wise reads (16 rows at one
+// piece) then meet 16 different slots of the 64 banks and transposed reads (8 rows of 4
+// pieces) each slot twice, the least; and a load from memory into LDS (64 lanes' pieces
+// in a row) takes the same pieces of 64 / PU rows in every unit.
 // ---------------------------------------------------------------------------
-template <int DT>
-constexpr int tile_stride(int W) {  // bytes
-  int s = W * esize<DT>() / 16;
-  while (!(s % 16 == 3 || s % 16 == 5 || s % 16 == 11 || s % 16 == 13)) ++s;
-  return 16 * s;
-}
 
 template <int DT>
-__device__ __forceinline__ void tile_put(char* t, int stride, int row, int col, const Frag<DT>& f) {
-  char* p = t + row * stride + col * esize<DT>();
-  *reinterpret_cast<u32x4*>(p) = f.v[0];
-  if constexpr (DT == kDtF32) *reinterpret_cast<u32x4*>(p + 16) = f.v[1];
+constexpr int pieces() {
+  return 2 * esize<DT>();
 }
-
+template <int DT>
+__device__ __forceinline__ int swz(int t) {
+  return DT == kDtF32 ? (t >> 1) & 7 : (t >> 2) & 3;
+}
+template <int DT, int R, int W>
+constexpr int tile_bytes() {
+  return R * W * esize<DT>();
+}
+// eight elements at row t, columns col .. col + 7
+template <int DT, int R>
+__device__ __forceinline__ void tile_put(char* tile, int t, int col, const Frag<DT>& f) {
+  constexpr int PU = pieces<DT>();
+  char* p = tile + ((col >> 5) * R + t) * PU * 16;
+  const int q = (col & 31) * esize<DT>() / 16, s = swz<DT>(t);
+  *reinterpret_cast<u32x4*>(p + 16 * (q ^ s)) = f.v[0];
+  if constexpr (DT == kDtF32) *reinterpret_cast<u32x4*>(p + 16 * ((q + 1) ^ s)) = f.v[1];
+}
 // A or B operand from rows: lane l takes row row0 + l % 32, columns col + 8 (l / 32) .. + 7
-template <int DT>
-__device__ __forceinline__ Frag<DT> frag_rows(const char* t, int stride, int row0, int col, int lane) {
-  const char* p = t + (row0 + (lane & 31)) * stride + (col + 8 * (lane >> 5)) * esize<DT>();
+// (row0 a multiple of 32, col of 16)
+template <int DT, int R>
+__device__ __forceinline__ Frag<DT> frag_rows(const char* tile, int row0, int col, int lane) {
+  constexpr int PU = pieces<DT>();
+  const int t = lane & 31, s = swz<DT>(t);
+  const char* p = tile + t * PU * 16;
+  const int o = ((col >> 5) * R + row0) * PU * 16;
   Frag<DT> f;
-  f.v[0] = *reinterpret_cast<const u32x4*>(p);
-  if constexpr (DT == kDtF32) f.v[1] = *reinterpret_cast<const u32x4*>(p + 16);
+  if constexpr (DT == kDtF32) {
+    const int q = 4 * ((col >> 4) & 1) + 2 * (lane >> 5);
+    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * (q ^ s) + o);
+    f.v[1] = *reinterpret_cast<const u32x4*>(p + 16 * ((q + 1) ^ s) + o);
+  } else {
+    const int q = 2 * ((col >> 4) & 1) + (lane >> 5);
+    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * (q ^ s) + o);
+  }
   return f;
 }
-
 // A operand from columns: lane l takes column col + l % 32 at rows row0 + 8 a + 4 (l / 32)
-// + b (slot 4 a + b).  16-bit types: two transposed reads (each 16-lane group takes
-// 4 rows x 16 columns).
-template <int DT>
-__device__ __forceinline__ Frag<DT> frag_cols(const char* t, int stride, int row0, int col, int lane) {
+// + b (slot 4 a + b); row0 a multiple of 16, col of 32.  16-bit types: two transposed
+// reads (each 16-lane group takes 4 rows x 16 columns).
+template <int DT, int R>
+__device__ __forceinline__ Frag<DT> frag_cols(const char* tile, int row0, int col, int lane) {
+  constexpr int PU = pieces<DT>();
+  const int u = lane >> 5, o = ((col >> 5) * R + row0) * PU * 16;
   Frag<DT> f;
-  const int u = lane >> 5;
   if constexpr (DT == kDtF32) {
-    const char* p = t + (row0 + 4 * u) * stride + (col + (lane & 31)) * 4;
+    const int q = (lane & 31) >> 2;
 #pragma unroll
-    for (int s = 0; s < 8; ++s)
-      f.v[s >> 2][s & 3] = *reinterpret_cast<const uint32_t*>(p + (8 * (s >> 2) + (s & 3)) * stride);
+    for (int k = 0; k < 8; ++k) {
+      const int t = 8 * (k >> 2) + 4 * u + (k & 3);  // (16 rows on, swz is the same)
+      f.v[k >> 2][k & 3] =
+          *reinterpret_cast<const uint32_t*>(tile + t * PU * 16 + 16 * (q ^ swz<DT>(t)) + 4 * (lane & 3) + o);
+    }
   } else {
     typedef __attribute__((address_space(3))) s16x4* lds4;
-    const int i = lane & 15, c = col + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
-    const char* p = t + (row0 + 4 * u + (i >> 2)) * stride + c * 2;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 8 * stride));
-    const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+    const int i = lane & 15, q = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1), t = 4 * u + (i >> 2);
+    const char* p0 = tile + t * PU * 16 + 16 * (q ^ swz<DT>(t)) + 8 * (i & 1);
+    const char* p1 = tile + (t + 8) * PU * 16 + 16 * (q ^ swz<DT>(t + 8)) + 8 * (i & 1);
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0 + o)));
+    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1 + o)));
     f.v[0] = u32x4{a[0], a[1], b[0], b[1]};
   }
   return f;
+}
+
+// 16 bytes of zeros that loads into LDS take for absent rows and columns
+__device__ const uint32_t kZeros[4] = {0u, 0u, 0u, 0u};
+
+// 64 lanes' 16 bytes each from memory into LDS at dst (the same for all lanes) + 16 lane.
+// Written as assembly (it has no output register) so that the compiler does not wait for it
+// before the next read of any LDS; wait_loads() does.  (Nothing else here uses m0.)
+__device__ __forceinline__ void load_lds16(const void* src, char* dst) {
+  const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)dst));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(off)), "v"(src)
+               : "memory");
+}
+
+// Memory and matrix instructions do not cross this point in the schedule (vector and
+// scalar ones may): it keeps a group's LDS reads ahead of the products with the group before.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }
+
+// A tile's rows of two joined parts (columns [0, n0) of p0 + row s0, then [n0, n0 + n1) of p1 +
+// row s1; element strides; zeros behind, and in rows from n_rows on) into LDS, by the
+// waves of a workgroup.  vec: as loads straight into LDS (16-byte pieces; the caller waits for
+// them), otherwise through registers.  One row address a lane and load row.
+template <int DT, int R, int W, int THREADS>
+__device__ __forceinline__ void tile_load(char* tile, const char* p0, int64_t s0, int n0, const char* p1, int64_t s1, int n1,
+                                          int n_rows, bool vec, int tid) {
+  constexpr int ES = esize<DT>(), PU = pieces<DT>(), TPL = 64 / PU, NW = THREADS / 64;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (vec) {
+    const char* zero = reinterpret_cast<const char*>(kZeros);
+#pragma unroll
+    for (int g = 0; g < R / TPL; g += NW) {
+      static_assert(R / TPL % NW == 0, "whole rounds of the waves");
+      const int gw = g + wave;
+      const int t = gw * TPL + lane / PU;
+      const int c = ((lane & (PU - 1)) ^ swz<DT>(t)) * (16 / ES);  // column within the unit
+      const bool ok = t < n_rows;
+      const char* a = p0 + t * s0 * ES + c * ES;
+      const char* b = n1 > 0 ? p1 + t * s1 * ES + (c - n0) * ES : a;
+#pragma unroll
+      for (int u = 0; u < W / 32; ++u) {
+        const int col = 32 * u + c;
+        const char* src = !ok || col >= n0 + n1 ? zero : col < n0 ? a + u * 32 * ES : b + u * 32 * ES;
+        load_lds16(src, tile + (u * R + gw * TPL) * PU * 16);
+      }
+    }
+  } else {
+    for (int u = tid; u < R * W / 8; u += THREADS) {
+      const int t = u / (W / 8), c = 8 * (u % (W / 8));
+      const Frag<DT> f =
+          t < n_rows ? load8_joined<DT>(p0 + t * s0 * ES, n0, p1 + t * s1 * ES, n1, c, false) : frag_zero<DT>();
+      tile_put<DT, R>(tile, t, c, f);
+    }
+  }
+}
+
+// a barrier for LDS: loads from memory stay in flight
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// this wave's loads from memory (into LDS too) have arrived
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xf70);  // vmcnt(0); LDS and scalar counters left alone
+  asm volatile("" ::: "memory");
 }
 
 // ---------------------------------------------------------------------------

@@ -22,9 +22,6 @@ namespace lb {
 
 namespace {
 
-typedef __attribute__((address_space(3))) void* lds_ptr;
-typedef __attribute__((address_space(1))) const void* glb_ptr;
-
 constexpr size_t kLdsMax = 163840;
 constexpr int kCols = 32;  // query rows of an item (columns of the tiles)
 constexpr int kG = 256;    // workgroups of split (one a CU)
@@ -438,15 +435,7 @@ struct SplitArgs {
   float* o;
 };
 
-// An LDS tile holds its tokens' columns of one wave, unit by unit: a unit's rows of PU
-// 16-byte pieces (4; fp32: 8), piece q of row t at q ^ swz(t).  Row-wise reads (16
-// rows at one piece) then meet 16 different slots of the 64 banks, transposed reads
-// (8 rows of 4 pieces) each slot twice, the least; and a lane loads the same one or
-// two places of every unit, 64 bytes of a row by four lanes.
-template <int CD>
-__device__ __forceinline__ int swz(int t) {
-  return CD == kDtF32 ? (t >> 1) & 7 : (t >> 2) & 3;
-}
+// An LDS tile holds its tokens' columns of one wave, unit by unit (attn_common.h).
 // row lane % tpt of a unit at columns 16 half + 8 (lane / 32) ..
 template <int CD>
 __device__ __forceinline__ Frag<CD> tile_rows(const char* unit, int tpt, int half, int lane) {
@@ -488,18 +477,6 @@ __device__ __forceinline__ Frag<CD> tile_cols(const char* t, int s, int lane) {
     f.v[0] = u32x4{a[0], a[1], b[0], b[1]};
   }
   return f;
-}
-
-// a barrier for LDS: loads from memory stay in flight
-__device__ __forceinline__ void lds_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-__device__ __forceinline__ void wait_loads() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xf70);  // vmcnt(0); LDS and scalar counters left alone
-  asm volatile("" ::: "memory");
 }
 
 template <int CD, int TQ, int TP, int UPW, bool CSPLIT>
@@ -576,8 +553,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 #pragma unroll
           for (int n = 0; n < NL; ++n) {
             if (n * TPL < p.tpt)
-              __builtin_amdgcn_global_load_lds((glb_ptr)(src[n] + u * 32 * ES),
-                                               (lds_ptr)(dst + (u * p.tpt + n * TPL) * PU * 16), 16, 0, 0);
+              load_lds16(src[n] + u * 32 * ES, dst + (u * p.tpt + n * TPL) * PU * 16);
           }
         }
       }
@@ -611,9 +587,8 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
       const int nf = 2 * nu * FP;
       for (int i = wave; i < TQ * nf; i += p.ntw) {
         const int n = i / nf, k = i - n * nf;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, (lds_ptr)(smem + (2 * n + 1) * p.tile_bytes + 1024 * k), 16,
-                                                 qo + (k / FP) * 16 * ES + (k % FP) * 16,
-                                                 n * static_cast<uint32_t>(row_bytes), 0, 0);
+        load_lds16(qbase + (rr * TQ + n) * row_bytes + (16 * (k / FP) + 8 * hh) * ES + 16 * (k % FP),
+                   smem + (2 * n + 1) * p.tile_bytes + 1024 * k);
       }
       wait_loads();
       lds_barrier();
