@@ -3,7 +3,7 @@
 //   P = exp(S - lse), D = rowsum(dO (.) O), dS = P (.) (dO V^T - D)
 //   dV = P^T dO, dK = scale dS^T Q_n, dK_rope = scale sum over heads dS^T Q_r, dQ = scale dS [K | K_rope]
 //
-// Two kernels, each forming S and dO V^T anew, so that every gradient is summed by
+// Two kernels (queries, then keys), each forming S and dO V^T anew, so that every gradient is summed by
 // one owner in a fixed order (no atomics on values): one owns 128 keys of a key head,
 // holds their K and V as B operands in registers and walks the queries of all heads
 // that share it; the other owns 128 queries and walks their keys.  The shared rotary
@@ -67,24 +67,207 @@ __global__ void __launch_bounds__(kThreads) delta_kernel(AttnArgs a, bool vec) {
   }
 }
 
+// S and dO V^T of a 32 x 32 block: A operands from rows of the tiles t0 (KC slices) and
+// t1 (2 VT slices), B operands in registers; groups of GK fragments, each read while the
+// one before is multiplied.
+template <int DT, int KC, int VC, int R>
+__device__ __forceinline__ void scores(const char* t0, const char* t1, int row0, int lane, const Frag<DT> (&b0)[KC],
+                                       const Frag<DT> (&b1)[VC], floatx16& s, floatx16& dp) {
+  constexpr int GK = DT == kDtF32 ? 1 : 4, N = KC + VC, NG = (N + GK - 1) / GK;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s[e] = 0.0f, dp[e] = 0.0f;
+  Frag<DT> f[2][GK];
+#pragma unroll
+  for (int g = -1; g < NG; ++g) {
+#pragma unroll
+    for (int n = 0; n < GK; ++n) {
+      const int c = (g + 1) * GK + n;
+      if (c < KC)
+        f[(g + 1) & 1][n] = frag_rows<DT, R>(t0, row0, 16 * c, lane);
+      else if (c < N)
+        f[(g + 1) & 1][n] = frag_rows<DT, R>(t1, row0, 16 * (c - KC), lane);
+    }
+    keep_order();
+    if (g >= 0) {
+#pragma unroll
+      for (int n = 0; n < GK; ++n) {
+        const int c = g * GK + n;
+        if (c < KC)
+          s = mma32<DT>(f[g & 1][n], b0[c < KC ? c : 0], s);
+        else if (c < N)
+          dp = mma32<DT>(f[g & 1][n], b1[c >= KC && c < N ? c - KC : 0], dp);
+      }
+    }
+  }
+}
+// acc[t] += (columns 32 t .. of the tile's rows row0 .. row0 + 31)^T x, x the block's
+// accumulator as B operand
+template <int DT, int T, int R>
+__device__ __forceinline__ void add_products(const char* tile, int row0, int lane, const floatx16& x, floatx16 (&acc)[T]) {
+  constexpr int GK = DT == kDtF32 ? 1 : T % 4 == 0 ? 4 : T % 3 == 0 ? 3 : 2, NG = 2 * T / GK;
+  Frag<DT> f[2][GK], xf[2];
+#pragma unroll
+  for (int sl = 0; sl < 2; ++sl) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = x[8 * sl + e];
+    xf[sl] = frag_from<DT>(v);
+  }
+#pragma unroll
+  for (int g = -1; g < NG; ++g) {
+    if (g + 1 < NG) {
+#pragma unroll
+      for (int n = 0; n < GK; ++n) {
+        const int c = (g + 1) * GK + n;
+        f[(g + 1) & 1][n] = frag_cols<DT, R>(tile, row0 + 16 * (c / T), 32 * (c % T), lane);
+      }
+    }
+    keep_order();
+    if (g >= 0) {
+#pragma unroll
+      for (int n = 0; n < GK; ++n) {
+        const int c = g * GK + n;
+        acc[c % T] = mma32<DT>(f[g & 1][n], xf[c / T], acc[c % T]);
+      }
+    }
+  }
+}
+
+// rows of a step: two tiles of 192 + 128 columns fill half of a CU's LDS
+template <int DT>
+constexpr int step_of() {
+  return DT == kDtF32 ? 32 : 64;
+}
+
+// queries: dQ.  For queries with few keys D is formed anew as sum_j P (dO V^T): the one
+// from the rounded O is off by up to half a step of it, which where few keys share the
+// weight is as large as the rounding of dS and the result together (at 20 keys 1.6 times
+// the result's own rounding, at 600 1.1 times).
+constexpr int kExactKeys = 512;
+template <int DT, int KC, int VT>
+__global__ void __launch_bounds__(kThreads, DT == kDtF32 || KC > 8 ? 1 : 2) attn_bwd_queries(BwdArgs f) {
+  constexpr int BN = step_of<DT>(), KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
+  constexpr int KB = tile_bytes<DT, BN, KW>(), TB = KB + tile_bytes<DT, BN, VW>(), ES = esize<DT>();
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const AttnArgs& a = f.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hh = lane >> 5, col = lane & 31;
+  const int id = blockIdx.x, hi_ = id % a.H, G = a.H / a.Hk;
+  const int kvh = hi_ % a.Hk, h = kvh * G + hi_ / a.Hk;
+  int seq, tile;
+  if (!find_tile(a.cu_q, a.n_seq, a.Tq, kBM, id / a.H, lane, seq, tile)) return;
+  seq = __builtin_amdgcn_readfirstlane(seq), tile = __builtin_amdgcn_readfirstlane(tile);
+  int q_lo, q_hi, k_lo, k_hi;
+  seq_range(a.cu_q, seq, a.Tq, q_lo, q_hi);
+  seq_range(a.cu_k, seq, a.Tk, k_lo, k_hi);
+  const int nq = q_hi - q_lo, nk = k_hi - k_lo, off = nk - nq;
+  tile = (nq + kBM - 1) / kBM - 1 - tile;  // the longest first
+  const int i0 = tile * kBM, i = i0 + 32 * wave + col;
+  const int dk = a.d_nope + a.d_rope, dv = a.d_v;
+  const int lim = a.causal ? min(nk - 1, i + off) : nk - 1;
+  const int lim_lo = a.causal ? min(nk - 1, i0 + 32 * wave + off) : nk - 1;
+  const int n_end = a.causal ? min(nk, min(i0 + kBM, nq) + off) : nk;
+  const int w_end = a.causal ? min(n_end, i0 + 32 * wave + 32 + off) : n_end;
+  const float sc = a.scale * kLog2e;
+  const float fac = ds_factor<DT>(a.top);
+
+  const char* kp = static_cast<const char*>(a.k) + (k_lo * a.k_t + kvh * a.k_h) * ES;
+  const char* vp = static_cast<const char*>(a.v) + (k_lo * a.v_t + kvh * a.v_h) * ES;
+  const char* rp = static_cast<const char*>(a.k_rope) + k_lo * a.kr_t * ES;
+  auto issue = [&](int j0, char* t) {
+    tile_load<DT, BN, KW, kThreads>(t, kp + j0 * a.k_t * ES, a.k_t, a.d_nope, rp + j0 * a.kr_t * ES, a.kr_t, a.d_rope,
+                                    nk - j0, f.vec, tid);
+    tile_load<DT, BN, VW, kThreads>(t + KB, vp + j0 * a.v_t * ES, a.v_t, dv, nullptr, 0, 0, nk - j0, f.vec, tid);
+  };
+  if (n_end > 0) issue(0, smem);
+  const int64_t row = static_cast<int64_t>(q_lo + min(i, nq - 1)) * a.H + h;
+  Frag<DT> qf[KC], df[2 * VT];
+  {
+    const char* qp = static_cast<const char*>(a.q) + ((q_lo + min(i, nq - 1)) * a.q_t + h * a.q_h) * ES;
+    const char* dp = static_cast<const char*>(a.d_o) + row * dv * ES;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) qf[c] = load8<DT>(qp, 16 * c + 8 * hh, dk, f.vec);
+#pragma unroll
+    for (int c = 0; c < 2 * VT; ++c) df[c] = load8<DT>(dp, 16 * c + 8 * hh, dv, f.vec);
+  }
+  const float l = a.lse[row];
+  float del = a.delta[row];
+  const float l2 = l == -INFINITY ? INFINITY : l * kLog2e;
+  // P in s, from S; the mask where the block reaches past a query's last key
+  auto probabilities = [&](int j, floatx16& s) {
+    const bool mask = j + 31 > lim_lo;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = exp2_fast(s[e] * sc - l2);
+      if (mask && j + 8 * (e >> 2) + 4 * hh + (e & 3) > lim) s[e] = 0.0f;
+    }
+  };
+  int at = 0;  // the tile that is read
+  // the keys' tiles in turn; the last step issues the first tile again if `more`
+  auto walk = [&](bool more, auto&& block) {
+    for (int j0 = 0; j0 < n_end; j0 += BN) {
+      char* kt = smem + at * TB;
+      at ^= 1;
+      wait_loads();
+      lds_barrier();
+      if (j0 + BN < n_end)
+        issue(j0 + BN, smem + at * TB);
+      else if (more)
+        issue(0, smem + at * TB);
+      if (j0 >= w_end) continue;
+#pragma unroll
+      for (int b = 0; b < BN / 32; ++b) block(kt, kt + KB, 32 * b, j0 + 32 * b);
+    }
+  };
+  if (n_end <= kExactKeys) {
+    float d = 0.0f;
+    walk(true, [&](const char* kt, const char* vt, int r0, int j) {
+      floatx16 s, dp;
+      scores<DT, KC, 2 * VT, BN>(kt, vt, r0, lane, qf, df, s, dp);
+      probabilities(j, s);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) d += s[e] == 0.0f ? 0.0f : s[e] * dp[e];
+    });
+    del = d + __shfl_xor(d, 32);
+    if (hh == 0 && i < nq) a.delta[row] = del;  // (read by the keys' kernel, which runs after this one)
+  }
+  floatx16 gq[KT];
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) gq[t][e] = 0.0f;
+  walk(false, [&](const char* kt, const char* vt, int r0, int j) {
+    floatx16 s, dp;
+    scores<DT, KC, 2 * VT, BN>(kt, vt, r0, lane, qf, df, s, dp);
+    probabilities(j, s);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dp[e] = s[e] == 0.0f ? 0.0f : s[e] * (dp[e] - del) * fac;
+    add_products<DT, KT, BN>(kt, r0, lane, dp, gq);
+  });
+  if (i >= nq) return;
+  const float qs = a.scale / fac;
+  char* gp = static_cast<char*>(a.dq) + row * dk * ES;
+#pragma unroll
+  for (int n = 0; n < KT; ++n)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      store4<DT>(gp, 32 * n + 2 * e + 4 * hh, dk, f.qvec, gq[n][e] * qs, gq[n][e + 1] * qs, gq[n][e + 2] * qs,
+                 gq[n][e + 3] * qs);
+}
+
 // keys: dK, dV
 template <int DT, int KC, int VT>
 __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
-  constexpr int BQ = DT == kDtF32 ? 32 : 64;  // queries of a step
-  constexpr int KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
-  constexpr int KS = tile_stride<DT>(KW), VS = tile_stride<DT>(VW);
-  constexpr int ES = esize<DT>();
+  constexpr int BQ = step_of<DT>(), KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
+  constexpr int KB = tile_bytes<DT, BQ, KW>(), TB = KB + tile_bytes<DT, BQ, VW>() + 8 * BQ, ES = esize<DT>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  char* qt = smem;
-  char* dt = smem + BQ * KS;
-  float* st_lse = reinterpret_cast<float*>(smem + BQ * (KS + VS));
-  float* st_del = st_lse + BQ;
   const AttnArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, col = lane & 31;
   const int kvh = blockIdx.x % a.Hk, G = a.H / a.Hk;
   int seq, tile;
   if (!find_tile(a.cu_k, a.n_seq, a.Tk, kBM, blockIdx.x / a.Hk, lane, seq, tile)) return;
+  seq = __builtin_amdgcn_readfirstlane(seq), tile = __builtin_amdgcn_readfirstlane(tile);
   int q_lo, q_hi, k_lo, k_hi;
   seq_range(a.cu_q, seq, a.Tq, q_lo, q_hi);
   seq_range(a.cu_k, seq, a.Tk, k_lo, k_hi);
@@ -94,6 +277,46 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
   const float sc = a.scale * kLog2e;
   const float fac = ds_factor<DT>(a.top);
 
+  const int i_begin = a.causal ? max(0, j0 - off) / BQ * BQ : 0;
+  const int n_it = max(0, (nq - i_begin + BQ - 1) / BQ), total = G * n_it;
+  // a step: the queries i0 .. of head g of the group
+  float lr = 0.0f, de = 0.0f;
+  auto issue = [&](int i0, int g, char* t) {
+    const int h = kvh * G + g;
+    tile_load<DT, BQ, KW, kThreads>(t, static_cast<const char*>(a.q) + ((q_lo + i0) * a.q_t + h * a.q_h) * ES, a.q_t, dk,
+                                    nullptr, 0, 0, nq - i0, f.vec, tid);
+    tile_load<DT, BQ, VW, kThreads>(
+        t + KB, static_cast<const char*>(a.d_o) + (static_cast<int64_t>(q_lo + i0) * a.H + h) * dv * ES,
+        static_cast<int64_t>(a.H) * dv, dv, nullptr, 0, 0, nq - i0, f.vec, tid);
+  };
+  // statistics of a step's queries: into registers, and a step later (when the loads have
+  // been waited for) into LDS
+  auto fetch_stats = [&](int i0, int g) {
+    if (tid < BQ) {
+      const int64_t r = static_cast<int64_t>(q_lo + min(i0 + tid, nq - 1)) * a.H + kvh * G + min(g, G - 1);
+      lr = a.lse[r], de = a.delta[r];
+    }
+  };
+  auto put_stats = [&](int i0, char* t) {
+    if (tid < BQ) {
+      // rows past the end and rows that see no key get probability 0
+      const bool ok = i0 + tid < nq && lr != -INFINITY;
+      float* st = reinterpret_cast<float*>(t + TB - 8 * BQ);
+      st[tid] = ok ? lr * kLog2e : INFINITY, st[BQ + tid] = ok ? de : 0.0f;
+    }
+  };
+  auto next = [&](int& i0, int& g) {
+    i0 += BQ;
+    if (i0 >= nq) i0 = i_begin, ++g;
+  };
+  int i1 = i_begin, g1 = 0;  // the step behind the current one
+  if (total > 0) {
+    fetch_stats(i1, g1);
+    put_stats(i1, smem);
+    issue(i1, g1, smem);
+    next(i1, g1);
+    fetch_stats(i1, g1);
+  }
   Frag<DT> kf[KC], vf[2 * VT];
   {
     const int64_t t = k_lo + min(j, nk - 1);
@@ -115,93 +338,45 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) gv[t][e] = 0.0f;
 
-  const int i_begin = a.causal ? max(0, j0 - off) / BQ * BQ : 0;
-  const int n_it = max(0, (nq - i_begin + BQ - 1) / BQ);
-  constexpr int QL = BQ * KW / 8 / kThreads, OL = BQ * VW / 8 / kThreads;
-  static_assert(QL * kThreads * 8 == BQ * KW && OL * kThreads * 8 == BQ * VW, "whole groups");
-  Frag<DT> qr[QL], dr_[OL];
-  float lr = 0.0f, de = 0.0f;
-  auto fetch = [&](int it) {  // step it of G * n_it: head it / n_it of the group
-    const int g = it / n_it, i0 = i_begin + (it - g * n_it) * BQ, h = kvh * G + g;
-#pragma unroll
-    for (int n = 0; n < QL; ++n) {
-      const int u = tid + n * kThreads, row = u / (KW / 8), c = 8 * (u % (KW / 8));
-      qr[n] = i0 + row < nq
-                  ? load8<DT>(static_cast<const char*>(a.q) + ((q_lo + i0 + row) * a.q_t + h * a.q_h) * ES, c, dk, f.vec)
-                  : frag_zero<DT>();
-    }
-#pragma unroll
-    for (int n = 0; n < OL; ++n) {
-      const int u = tid + n * kThreads, row = u / (VW / 8), c = 8 * (u % (VW / 8));
-      dr_[n] = i0 + row < nq ? load8<DT>(static_cast<const char*>(a.d_o) +
-                                             (static_cast<int64_t>(q_lo + i0 + row) * a.H + h) * dv * ES,
-                                         c, dv, f.vec)
-                             : frag_zero<DT>();
-    }
-    if (tid < BQ) {
-      const bool ok = i0 + tid < nq;
-      const int64_t r = static_cast<int64_t>(q_lo + min(i0 + tid, nq - 1)) * a.H + h;
-      const float l = a.lse[r];
-      // rows past the end and rows that see no key get probability 0
-      lr = ok && l != -INFINITY ? l * kLog2e : INFINITY;
-      de = ok ? a.delta[r] : 0.0f;
-    }
-  };
-  const int total = G * n_it;
-  if (total > 0) fetch(0);
+  int i_now = i_begin;
   for (int it = 0; it < total; ++it) {
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < QL; ++n) {
-      const int u = tid + n * kThreads;
-      tile_put<DT>(qt, KS, u / (KW / 8), 8 * (u % (KW / 8)), qr[n]);
+    const char* qt = smem + (it & 1) * TB;
+    const char* dt = qt + KB;
+    const float* st = reinterpret_cast<const float*>(qt + TB - 8 * BQ);
+    wait_loads();
+    lds_barrier();
+    const int i_here = i_now;
+    i_now = i1;
+    if (it + 1 < total) {
+      char* t = smem + (~it & 1) * TB;
+      put_stats(i1, t);
+      const int ii = i1, gi = g1;
+      next(i1, g1);
+      fetch_stats(i1, g1);
+      issue(ii, gi, t);
     }
-#pragma unroll
-    for (int n = 0; n < OL; ++n) {
-      const int u = tid + n * kThreads;
-      tile_put<DT>(dt, VS, u / (VW / 8), 8 * (u % (VW / 8)), dr_[n]);
-    }
-    if (tid < BQ) st_lse[tid] = lr, st_del[tid] = de;
-    __syncthreads();
-    const int i0 = i_begin + it % n_it * BQ;
-    if (it + 1 < total) fetch(it + 1);
+    if (a.causal && i_here + BQ - 1 + off < j0 + 32 * wave) continue;  // every query before the wave's first key
 #pragma unroll
     for (int b = 0; b < BQ / 32; ++b) {
       floatx16 s, dp;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.0f, dp[e] = 0.0f;
-#pragma unroll
-      for (int c = 0; c < KC; ++c) s = mma32<DT>(frag_rows<DT>(qt, KS, 32 * b, 16 * c, lane), kf[c], s);
-#pragma unroll
-      for (int c = 0; c < 2 * VT; ++c) dp = mma32<DT>(frag_rows<DT>(dt, VS, 32 * b, 16 * c, lane), vf[c], dp);
-      const bool mask = a.causal && i0 + 32 * b + off < j0 + 32 * wave + 31;
+      scores<DT, KC, 2 * VT, BQ>(qt, dt, 32 * b, lane, kf, vf, s, dp);
+      const bool mask = a.causal && i_here + 32 * b + off < j0 + 32 * wave + 31;
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
         const int row = 32 * b + 2 * e + 4 * hh;
-        const float4 l4 = *reinterpret_cast<const float4*>(st_lse + row);
-        const float4 d4 = *reinterpret_cast<const float4*>(st_del + row);
+        const float4 l4 = *reinterpret_cast<const float4*>(st + row);
+        const float4 d4 = *reinterpret_cast<const float4*>(st + BQ + row);
         const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           float p = exp2_fast(s[e + q] * sc - lv[q]);
-          if (mask && i0 + row + q + off < j) p = 0.0f;
+          if (mask && i_here + row + q + off < j) p = 0.0f;
           s[e + q] = p;
           dp[e + q] = p == 0.0f ? 0.0f : p * (dp[e + q] - dl[q]) * fac;
         }
       }
-#pragma unroll
-      for (int sl = 0; sl < 2; ++sl) {
-        float x[8], y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = s[8 * sl + e], y[e] = dp[8 * sl + e];
-        const Frag<DT> pf = frag_from<DT>(x), df = frag_from<DT>(y);
-#pragma unroll
-        for (int t = 0; t < VT; ++t)
-          gv[t] = mma32<DT>(frag_cols<DT>(dt, VS, 32 * b + 16 * sl, 32 * t, lane), pf, gv[t]);
-#pragma unroll
-        for (int t = 0; t < KT; ++t)
-          gk[t] = mma32<DT>(frag_cols<DT>(qt, KS, 32 * b + 16 * sl, 32 * t, lane), df, gk[t]);
-      }
+      add_products<DT, VT, BQ>(dt, 32 * b, lane, s, gv);
+      add_products<DT, KT, BQ>(qt, 32 * b, lane, dp, gk);
     }
   }
   if (j >= nk) return;
@@ -227,128 +402,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
     }
 }
 
-// queries: dQ
-template <int DT, int KC, int VT>
-__global__ void __launch_bounds__(kThreads, 1) attn_bwd_queries(BwdArgs f) {
-  constexpr int BN = DT == kDtF32 ? 32 : 64;  // keys of a step
-  constexpr int KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
-  constexpr int KS = tile_stride<DT>(KW), VS = tile_stride<DT>(VW);
-  constexpr int ES = esize<DT>();
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  char* kt = smem;
-  char* vt = smem + BN * KS;
-  const AttnArgs& a = f.a;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int hh = lane >> 5, col = lane & 31;
-  const int id = blockIdx.x, hi_ = id % a.H, G = a.H / a.Hk;
-  const int kvh = hi_ % a.Hk, h = kvh * G + hi_ / a.Hk;
-  int seq, tile;
-  if (!find_tile(a.cu_q, a.n_seq, a.Tq, kBM, id / a.H, lane, seq, tile)) return;
-  int q_lo, q_hi, k_lo, k_hi;
-  seq_range(a.cu_q, seq, a.Tq, q_lo, q_hi);
-  seq_range(a.cu_k, seq, a.Tk, k_lo, k_hi);
-  const int nq = q_hi - q_lo, nk = k_hi - k_lo, off = nk - nq;
-  tile = (nq + kBM - 1) / kBM - 1 - tile;  // the longest first
-  const int i0 = tile * kBM, i = i0 + 32 * wave + col;
-  const int dk = a.d_nope + a.d_rope, dv = a.d_v;
-  const int lim = a.causal ? min(nk - 1, i + off) : nk - 1;
-  const int lim_lo = a.causal ? min(nk - 1, i0 + 32 * wave + off) : nk - 1;
-  const int n_end = a.causal ? min(nk, min(i0 + kBM, nq) + off) : nk;
-  const float sc = a.scale * kLog2e;
-  const float fac = ds_factor<DT>(a.top);
-
-  const int64_t row = static_cast<int64_t>(q_lo + min(i, nq - 1)) * a.H + h;
-  Frag<DT> qf[KC], df[2 * VT];
-  {
-    const char* qp = static_cast<const char*>(a.q) + ((q_lo + min(i, nq - 1)) * a.q_t + h * a.q_h) * ES;
-    const char* dp = static_cast<const char*>(a.d_o) + row * dv * ES;
-#pragma unroll
-    for (int c = 0; c < KC; ++c) qf[c] = load8<DT>(qp, 16 * c + 8 * hh, dk, f.vec);
-#pragma unroll
-    for (int c = 0; c < 2 * VT; ++c) df[c] = load8<DT>(dp, 16 * c + 8 * hh, dv, f.vec);
-  }
-  const float l = a.lse[row], del = a.delta[row];
-  const float l2 = l == -INFINITY ? INFINITY : l * kLog2e;
-  floatx16 gq[KT];
-#pragma unroll
-  for (int t = 0; t < KT; ++t)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) gq[t][e] = 0.0f;
-
-  constexpr int KL = BN * KW / 8 / kThreads, VL = BN * VW / 8 / kThreads;
-  static_assert(KL * kThreads * 8 == BN * KW && VL * kThreads * 8 == BN * VW, "whole groups");
-  Frag<DT> kr[KL], vr[VL];
-  const char* kp = static_cast<const char*>(a.k) + kvh * a.k_h * ES;
-  const char* vp = static_cast<const char*>(a.v) + kvh * a.v_h * ES;
-  const char* rp = static_cast<const char*>(a.k_rope);
-  auto fetch = [&](int j0) {
-#pragma unroll
-    for (int n = 0; n < KL; ++n) {
-      const int u = tid + n * kThreads, r = u / (KW / 8), c = 8 * (u % (KW / 8));
-      const int64_t t = k_lo + j0 + r;
-      kr[n] = j0 + r < nk ? load8_joined<DT>(kp + t * a.k_t * ES, a.d_nope, rp + t * a.kr_t * ES, a.d_rope, c, f.vec)
-                          : frag_zero<DT>();
-    }
-#pragma unroll
-    for (int n = 0; n < VL; ++n) {
-      const int u = tid + n * kThreads, r = u / (VW / 8), c = 8 * (u % (VW / 8));
-      vr[n] = j0 + r < nk ? load8<DT>(vp + (k_lo + j0 + r) * a.v_t * ES, c, dv, f.vec) : frag_zero<DT>();
-    }
-  };
-  if (n_end > 0) fetch(0);
-  for (int j0 = 0; j0 < n_end; j0 += BN) {
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < KL; ++n) {
-      const int u = tid + n * kThreads;
-      tile_put<DT>(kt, KS, u / (KW / 8), 8 * (u % (KW / 8)), kr[n]);
-    }
-#pragma unroll
-    for (int n = 0; n < VL; ++n) {
-      const int u = tid + n * kThreads;
-      tile_put<DT>(vt, VS, u / (VW / 8), 8 * (u % (VW / 8)), vr[n]);
-    }
-    __syncthreads();
-    if (j0 + BN < n_end) fetch(j0 + BN);
-#pragma unroll
-    for (int b = 0; b < BN / 32; ++b) {
-      floatx16 s, dp;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.0f, dp[e] = 0.0f;
-#pragma unroll
-      for (int c = 0; c < KC; ++c) s = mma32<DT>(frag_rows<DT>(kt, KS, 32 * b, 16 * c, lane), qf[c], s);
-#pragma unroll
-      for (int c = 0; c < 2 * VT; ++c) dp = mma32<DT>(frag_rows<DT>(vt, VS, 32 * b, 16 * c, lane), df[c], dp);
-      const bool mask = j0 + 32 * b + 31 > lim_lo;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        float p = exp2_fast(s[e] * sc - l2);
-        if (mask && j0 + 32 * b + 8 * (e >> 2) + 4 * hh + (e & 3) > lim) p = 0.0f;
-        dp[e] = p == 0.0f ? 0.0f : p * (dp[e] - del) * fac;
-      }
-#pragma unroll
-      for (int sl = 0; sl < 2; ++sl) {
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = dp[8 * sl + e];
-        const Frag<DT> sf = frag_from<DT>(y);
-#pragma unroll
-        for (int t = 0; t < KT; ++t)
-          gq[t] = mma32<DT>(frag_cols<DT>(kt, KS, 32 * b + 16 * sl, 32 * t, lane), sf, gq[t]);
-      }
-    }
-  }
-  if (i >= nq) return;
-  const float qs = a.scale / fac;
-  char* gp = static_cast<char*>(a.dq) + row * dk * ES;
-#pragma unroll
-  for (int n = 0; n < KT; ++n)
-#pragma unroll
-    for (int e = 0; e < 16; e += 4)
-      store4<DT>(gp, 32 * n + 2 * e + 4 * hh, dk, f.qvec, gq[n][e] * qs, gq[n][e + 1] * qs, gq[n][e + 2] * qs,
-                 gq[n][e + 3] * qs);
-}
-
 // the shared rotary key's gradient: the key heads' partial results in order
 template <int DT>
 __global__ void __launch_bounds__(kThreads) rope_sum(AttnArgs a) {
@@ -365,22 +418,22 @@ __global__ void __launch_bounds__(kThreads) rope_sum(AttnArgs a) {
 
 template <int DT, int KC, int VT>
 hipError_t bwd_launch(const BwdArgs& f, hipStream_t stream) {
-  constexpr int B = DT == kDtF32 ? 32 : 64;
-  constexpr size_t tiles = static_cast<size_t>(B) * (tile_stride<DT>(16 * KC) + tile_stride<DT>(32 * VT));
+  constexpr int B = step_of<DT>();
+  constexpr size_t tiles = 2 * static_cast<size_t>(tile_bytes<DT, B, 16 * KC + 32 * VT>()), stats = 2 * 8 * B;
   static LdsLimit lk, lq;
-  hipError_t e = raise_lds(reinterpret_cast<const void*>(&attn_bwd_keys<DT, KC, VT>), tiles + 8 * B, lk);
+  hipError_t e = raise_lds(reinterpret_cast<const void*>(&attn_bwd_keys<DT, KC, VT>), tiles + stats, lk);
   if (e != hipSuccess) return e;
   e = raise_lds(reinterpret_cast<const void*>(&attn_bwd_queries<DT, KC, VT>), tiles, lq);
   if (e != hipSuccess) return e;
-  if (f.tiles_k > 0) {
-    hipLaunchKernelGGL((attn_bwd_keys<DT, KC, VT>), dim3(static_cast<uint32_t>(f.tiles_k) * f.a.Hk), dim3(kThreads),
-                       tiles + 8 * B, stream, f);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   if (f.tiles_q > 0) {
     hipLaunchKernelGGL((attn_bwd_queries<DT, KC, VT>), dim3(static_cast<uint32_t>(f.tiles_q) * f.a.H), dim3(kThreads),
                        tiles, stream, f);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (f.tiles_k > 0) {
+    hipLaunchKernelGGL((attn_bwd_keys<DT, KC, VT>), dim3(static_cast<uint32_t>(f.tiles_k) * f.a.Hk), dim3(kThreads),
+                       tiles + stats, stream, f);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
