@@ -70,10 +70,10 @@ __global__ void __launch_bounds__(kThreads) delta_kernel(AttnArgs a, bool vec) {
 // S and dO V^T of a 32 x 32 block: A operands from rows of the tiles t0 (KC slices) and
 // t1 (2 VT slices), B operands in registers; groups of GK fragments, each read while the
 // one before is multiplied.
-template <int DT, int KC, int VC, int R>
+template <int DT, int KC, int VC, int R, int GK = (DT == kDtF32 ? 1 : 4)>
 __device__ __forceinline__ void scores(const char* t0, const char* t1, int row0, int lane, const Frag<DT> (&b0)[KC],
                                        const Frag<DT> (&b1)[VC], floatx16& s, floatx16& dp) {
-  constexpr int GK = DT == kDtF32 ? 1 : 4, N = KC + VC, NG = (N + GK - 1) / GK;
+  constexpr int N = KC + VC, NG = (N + GK - 1) / GK;
 #pragma unroll
   for (int e = 0; e < 16; ++e) s[e] = 0.0f, dp[e] = 0.0f;
   Frag<DT> f[2][GK];
@@ -102,9 +102,9 @@ __device__ __forceinline__ void scores(const char* t0, const char* t1, int row0,
 }
 // acc[t] += (columns 32 t .. of the tile's rows row0 .. row0 + 31)^T x, x the block's
 // accumulator as B operand
-template <int DT, int T, int R>
+template <int DT, int T, int R, int MOST = 4>
 __device__ __forceinline__ void add_products(const char* tile, int row0, int lane, const floatx16& x, floatx16 (&acc)[T]) {
-  constexpr int GK = DT == kDtF32 ? 1 : T % 4 == 0 ? 4 : T % 3 == 0 ? 3 : 2, NG = 2 * T / GK;
+  constexpr int GK = DT == kDtF32 ? 1 : T % 4 == 0 && MOST >= 4 ? 4 : T % 3 == 0 && MOST >= 3 ? 3 : 2, NG = 2 * T / GK;
   Frag<DT> f[2][GK], xf[2];
 #pragma unroll
   for (int sl = 0; sl < 2; ++sl) {
@@ -145,8 +145,9 @@ constexpr int step_of() {
 // the result's own rounding, at 600 1.1 times).
 constexpr int kExactKeys = 512;
 template <int DT, int KC, int VT>
-__global__ void __launch_bounds__(kThreads, DT == kDtF32 || KC > 8 ? 1 : 2) attn_bwd_queries(BwdArgs f) {
+__global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_bwd_queries(BwdArgs f) {
   constexpr int BN = step_of<DT>(), KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
+  constexpr int SG = DT == kDtF32 ? 1 : KC > 8 ? 2 : 4;  // fragments read ahead: two waves a SIMD leave 256 registers
   constexpr int KB = tile_bytes<DT, BN, KW>(), TB = KB + tile_bytes<DT, BN, VW>(), ES = esize<DT>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const AttnArgs& a = f.a;
@@ -223,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || KC > 8 ? 1 : 2) attn
     float d = 0.0f;
     walk(true, [&](const char* kt, const char* vt, int r0, int j) {
       floatx16 s, dp;
-      scores<DT, KC, 2 * VT, BN>(kt, vt, r0, lane, qf, df, s, dp);
+      scores<DT, KC, 2 * VT, BN, SG>(kt, vt, r0, lane, qf, df, s, dp);
       probabilities(j, s);
 #pragma unroll
       for (int e = 0; e < 16; ++e) d += s[e] == 0.0f ? 0.0f : s[e] * dp[e];
@@ -238,11 +239,11 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || KC > 8 ? 1 : 2) attn
     for (int e = 0; e < 16; ++e) gq[t][e] = 0.0f;
   walk(false, [&](const char* kt, const char* vt, int r0, int j) {
     floatx16 s, dp;
-    scores<DT, KC, 2 * VT, BN>(kt, vt, r0, lane, qf, df, s, dp);
+    scores<DT, KC, 2 * VT, BN, SG>(kt, vt, r0, lane, qf, df, s, dp);
     probabilities(j, s);
 #pragma unroll
     for (int e = 0; e < 16; ++e) dp[e] = s[e] == 0.0f ? 0.0f : s[e] * (dp[e] - del) * fac;
-    add_products<DT, KT, BN>(kt, r0, lane, dp, gq);
+    add_products<DT, KT, BN, SG>(kt, r0, lane, dp, gq);
   });
   if (i >= nq) return;
   const float qs = a.scale / fac;
