@@ -92,7 +92,7 @@ __host__ LatWs lat_ws(int64_t T, int64_t n_seq, int64_t H, int r, int d_rope) {
   const int64_t row = latent_row(r, d_rope), ow = (2 * r + 31) / 32 * 32;
   const int64_t slots = kG + (T * H + kCols - 1) / kCols + n_seq;
   auto up = [](size_t b) { return (b + 255) / 256 * 256; };
-  w.qs_off = up(static_cast<size_t>(T * H * row) * 6);
+  w.qs_off = up(static_cast<size_t>((T * H + kCols - 1) / kCols * kCols * row) * 6);
   w.ml_off = w.qs_off + up(static_cast<size_t>(T * H) * 4);
   w.o_off = w.ml_off + up(static_cast<size_t>(slots) * kCols * 8);
   w.bytes = w.o_off + up(static_cast<size_t>(slots) * kCols * ow * 4);
@@ -257,6 +257,15 @@ constexpr int kMaxHead = 256;    // widths of a head
 constexpr int kRopeHeads = 8;    // heads of a rotary workgroup
 constexpr int kAbsTokens = 32;   // tokens of a tile
 
+// q' is kept as the B operands that split reads: for every 32 rows m = t H + h, term and
+// 16-byte piece of the row's columns, the 32 rows' pieces next to each other.  Bytes from
+// the start to column col of term n of row m:
+template <int CD, int TQ>
+__device__ __forceinline__ int64_t q_offset(int64_t m, int n, int col, int row) {
+  constexpr int EP = 16 / esize<CD>();  // elements of a piece
+  return (((m >> 5) * TQ + n) * (row / EP) + col / EP) * 512 + (m & 31) * 16 + col % EP * esize<CD>();
+}
+
 // With an f16 cache q' is brought into f16's range by a power of two per row: the
 // inverse of a bound on the row's values (order-free maxima, so that every workgroup
 // finds the same one).  top: the largest |h (.) q|, rope: of the rotary part.
@@ -278,7 +287,6 @@ __global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout
   const int lane = threadIdx.x, hh = lane >> 5;
   const CacheArgs& c = a.c;
   const int r = c.r, dn = a.d_nope, dr = c.d_rope, row = c.row, G = a.H / a.Hk;
-  constexpr int ES = esize<CD>();
   if (static_cast<int>(blockIdx.x) < n_mma) {
     const int u = blockIdx.x % (2 * nkb), hb = blockIdx.x / (2 * nkb), h = hb % a.H, t0 = hb / a.H * kAbsTokens;
     const int p = u >= nkb, kb = u - p * nkb, i0 = h / G * dn;
@@ -354,11 +362,11 @@ __global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout
       float x = acc[e];
       if constexpr (CD == kDtF16) x *= __shfl(f, tt);
       if (t0 + tt < a.T && k < r) {
-        char* o = qout + ((static_cast<int64_t>(t0 + tt) * a.H + h) * TQ * row + p * r + k) * ES;
+        const int64_t m = static_cast<int64_t>(t0 + tt) * a.H + h;
 #pragma unroll
         for (int n = 0; n < TQ; ++n) {
           const float y = rounded<CD>(x);
-          st<CD>(o + static_cast<int64_t>(n) * row * ES, 0, y);
+          st<CD>(qout + q_offset<CD, TQ>(m, n, p * r + k, row), 0, y);
           x -= y;
         }
       }
@@ -374,26 +382,27 @@ __global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout
     int sb, ib;
     if (map.find(false, t, s, sb, ib) >= 0) pos = max(0, s.len - s.nq + (t - s.q0));
   }
-  float f[kRopeHeads];
+  float f = 1.0f;  // of head h0 + lane / 8
+  if constexpr (CD == kDtF16) {
+    const int h = min(h0 + lane / 8, a.H - 1), i0 = h / G * dn;
+    const char* q = static_cast<const char*>(a.q) + (t * a.q_t + h * a.q_h) * esize<DT>();
+    float top = 0.0f, rope = 0.0f;
+    for (int i = 8 * (lane & 7); i < dn; i += 64) {
+      const Frag<DT> x = load8<DT>(q, i, dn, vec);
+      const Frag<SC> y = load8<SC>(static_cast<const char*>(a.h[0]) + i0 * esize<SC>(), i, dn, vec);
+      const Frag<SC> z = load8<SC>(static_cast<const char*>(a.h[1]) + i0 * esize<SC>(), i, dn, vec);
 #pragma unroll
-  for (int n = 0; n < kRopeHeads; ++n) {
-    f[n] = 1.0f;
-    if (h0 + n >= h1) continue;
-    if constexpr (CD == kDtF16) {
-      const char* q = static_cast<const char*>(a.q) + (t * a.q_t + (h0 + n) * a.q_h) * esize<DT>();
-      const int i0 = (h0 + n) / G * dn;
-      float top = 0.0f, rope = 0.0f;
-      for (int i = lane; i < dn; i += 64) {
-        const float qe = ld<DT>(q, i);
-        top = fmaxf(top, fmaxf(fabsf(qe * ld<SC>(a.h[0], i0 + i)), fabsf(qe * ld<SC>(a.h[1], i0 + i))));
+      for (int e = 0; e < 8; ++e) {
+        const float qe = frag_elem<DT>(x, e);
+        top = fmaxf(top, fmaxf(fabsf(qe * frag_elem<SC>(y, e)), fabsf(qe * frag_elem<SC>(z, e))));
       }
-      for (int i = lane; i < dr; i += 64) rope = fmaxf(rope, fabsf(ld<DT>(q, dn + i)));
-#pragma unroll
-      for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s)), rope = fmaxf(rope, __shfl_xor(rope, s));
-      f[n] = row_factor(top, rope, dn);
     }
-    if (lane == 0) qsc[static_cast<int64_t>(t) * a.H + h0 + n] = a.scale * kLog2e / f[n];
+    for (int i = lane & 7; i < dr; i += 8) rope = fmaxf(rope, fabsf(ld<DT>(q, dn + i)));
+#pragma unroll
+    for (int s = 4; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s)), rope = fmaxf(rope, __shfl_xor(rope, s));
+    f = row_factor(top, rope, dn);
   }
+  if ((lane & 7) == 0 && h0 + lane / 8 < h1) qsc[static_cast<int64_t>(t) * a.H + h0 + lane / 8] = a.scale * kLog2e / f;
   const int half = dr / 2;
   for (int i = lane; i < row - 2 * r; i += 64) {
     const bool in = i < dr, low = i < half;
@@ -409,12 +418,11 @@ __global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout
         x = ld<DT>(q, dn + i);
         if (a.freqs != nullptr) x = x * cs + ld<DT>(q, dn + (low ? i + half : i - half)) * sn;
       }
-      x *= f[n];
-      char* o = qout + ((static_cast<int64_t>(t) * a.H + h0 + n) * TQ * row + 2 * r + i) * ES;
+      if constexpr (CD == kDtF16) x *= __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), 8 * n));
 #pragma unroll
       for (int m = 0; m < TQ; ++m) {
         const float y = rounded<CD>(x);
-        st<CD>(o + static_cast<int64_t>(m) * row * ES, 0, y);
+        st<CD>(qout + q_offset<CD, TQ>(static_cast<int64_t>(t) * a.H + h0 + n, m, 2 * r + i, row), 0, y);
         x -= y;
       }
     }
@@ -576,19 +584,18 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
     const int pos = first + quotient(item * kCols + rr, a.heads);
     const int pos_min = first + quotient(item * kCols, a.heads);
     const float qs = a.qsc[m0 + rr];
-    const char* qbase = a.q + m0 * TQ * row_bytes + u0 * 32 * ES;
-    const rsrc_t qr = make_rsrc_uniform(qbase, kCols * TQ * static_cast<uint32_t>(row_bytes));
-    const uint32_t qo = rr * TQ * static_cast<uint32_t>(row_bytes) + 8 * hh * ES;
+    // (piece of 16 bytes: slice k of 16 columns, the lane's half of it, part f of an fp32 eight)
+    const char* qbase = a.q + q_offset<CD, TQ>(m0 + rr, 0, 32 * u0 + 8 * hh, c.row);
+    const int term = c.row / (16 / ES) * 512;
     Frag<CD> qf[2 * UPW][TQ];
-    constexpr int FP = ES / 2;  // 16-byte pieces of a fragment a lane
+    constexpr int FP = ES / 2;  // pieces of a fragment a lane
     if (!CSPLIT && p.stages == 2 && p.ntw >= TQ) {
       // the token waves need the same fragments: each loads a part of them into the second
       // tiles (term n into wave n's), and all read them from there
       const int nf = 2 * nu * FP;
       for (int i = wave; i < TQ * nf; i += p.ntw) {
         const int n = i / nf, k = i - n * nf;
-        load_lds16(qbase + (rr * TQ + n) * row_bytes + (16 * (k / FP) + 8 * hh) * ES + 16 * (k % FP),
-                   smem + (2 * n + 1) * p.tile_bytes + 1024 * k);
+        load_lds16(qbase + n * term + (k / FP) * 1024 * FP + k % FP * 512, smem + (2 * n + 1) * p.tile_bytes + 1024 * k);
       }
       wait_loads();
       lds_barrier();
@@ -612,10 +619,9 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
         for (int n = 0; n < TQ; ++n) {
           qf[k][n] = frag_zero<CD>();
           if (EXACT || k < 2 * nu) {
-            const uint32_t so = n * static_cast<uint32_t>(row_bytes);
-            qf[k][n].v[0] = __builtin_amdgcn_raw_buffer_load_b128(qr, qo + 16 * k * ES, so, 0);
-            if constexpr (CD == kDtF32)
-              qf[k][n].v[1] = __builtin_amdgcn_raw_buffer_load_b128(qr, qo + 16 * k * ES + 16, so, 0);
+            const char* src = qbase + n * term + k * 1024 * FP;
+            qf[k][n].v[0] = *reinterpret_cast<const u32x4*>(src);
+            if constexpr (CD == kDtF32) qf[k][n].v[1] = *reinterpret_cast<const u32x4*>(src + 512);
           }
         }
       }
@@ -734,13 +740,29 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
     float* po = a.o + slot * kCols * ow;
     float* pm = a.ml + slot * kCols * 2;
     if constexpr (CSPLIT) {
+      // two units at a time through the wave's tile, so that rows are written 256 bytes at a time
+      constexpr int st = 68;  // floats of a row there
+      float* buf = reinterpret_cast<float*>(tiles);
+      asm volatile("" ::: "memory");
 #pragma unroll
-      for (int u = 0; u < UPW; ++u) {
+      for (int u = 0; u < UPW; u += 2) {
         if (u < vu) {
 #pragma unroll
-          for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<float4*>(po + ml_ * ow + 32 * (u0 + u) + 2 * e + 4 * hh) =
-                make_float4(o[u][e], o[u][e + 1], o[u][e + 2], o[u][e + 3]);
+          for (int v = 0; v < 2; ++v) {
+            if (u + v < UPW) {
+#pragma unroll
+              for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<float4*>(buf + ml_ * st + 32 * v + 2 * e + 4 * hh) =
+                    make_float4(o[u + v][e], o[u + v][e + 1], o[u + v][e + 2], o[u + v][e + 3]);
+            }
+          }
+          const int c4 = 4 * (lane & 15);
+#pragma unroll
+          for (int n = 0; n < 8; ++n) {
+            const int m = 4 * n + (lane >> 4);
+            if (32 * u + c4 < 32 * vu)
+              *reinterpret_cast<float4*>(po + m * ow + 32 * (u0 + u) + c4) = *reinterpret_cast<const float4*>(buf + m * st + c4);
+          }
         }
       }
       if (wave == 0 && hh == 0) pm[2 * ml_] = mx, pm[2 * ml_ + 1] = sum;
@@ -805,26 +827,26 @@ struct JoinArgs {
 
 // A workgroup per (token, head): the partial sums of its row, in workgroup order,
 // then its head's rows of U with h.
-template <int DT, int SC, int kMaxHalf, int kJThreads>
+template <int DT, int SC, int KPARTS, int kMaxHalf, int kJThreads>
 __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
   __shared__ float wt[256];
   __shared__ __attribute__((aligned(16))) float ov[2][kMaxLatentRank];
-  __shared__ float part[2][2][kMaxHead];
+  __shared__ float part[KPARTS][2][kMaxHead];
   const LatentAttnArgs& a = j.a;
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63;
   const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H;
   const int step = j.p.step, r = c.r, rp = (r + 31) & ~31;
-  // the words of this thread's output, path and half of the path's words: they do not
+  // the words of this thread's output, path and part of the path's words: they do not
   // depend on the sums
   const int n_out = a.Hk * (a.d_nope + a.d_v), row0 = a.Hk * a.d_nope + h / (a.H / a.Hk) * a.d_v;
-  const int nb2 = (rp / 32 + 1) / 2;
+  const int nb2 = (rp / 32 + KPARTS - 1) / KPARTS;
   uint32_t words[kMaxHalf];
   const int ph = tid / a.d_v, wp = ph & 1, wi = tid - ph * a.d_v, wk = (ph >> 1) * nb2;
 #pragma unroll
   for (int n = 0; n < kMaxHalf; ++n) {
     // (the last one may be of 16 bits; absent ones read the first word again)
-    const bool ok = ph < 4 && n < nb2 && wk + n < rp / 32;
+    const bool ok = ph < 2 * KPARTS && n < nb2 && wk + n < rp / 32;
     words[n] = word_at(word_column(a.U[wp], n_out, r, ok ? wk + n : 0), ok ? row0 + wi : 0);
   }
   WorkMap map{c, a.T, a.H, step, lane};
@@ -871,7 +893,7 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
     ov[k >= r][k >= r ? k - r : k] = v * inv;
   }
   __syncthreads();
-  if (ph < 4) {
+  if (ph < 2 * KPARTS) {
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < kMaxHalf; ++n) {
@@ -889,8 +911,10 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
   }
   __syncthreads();
   for (int i = tid; i < a.d_v; i += kJThreads) {
-    const float y0 = ld<SC>(a.h[0], row0 + i) * (part[0][0][i] + part[1][0][i]);
-    const float y1 = ld<SC>(a.h[1], row0 + i) * (part[0][1][i] + part[1][1][i]);
+    float s0 = part[0][0][i], s1 = part[0][1][i];
+#pragma unroll
+    for (int n = 1; n < KPARTS; ++n) s0 += part[n][0][i], s1 += part[n][1][i];
+    const float y0 = ld<SC>(a.h[0], row0 + i) * s0, y1 = ld<SC>(a.h[1], row0 + i) * s1;
     st<DT>(out, i, y0 + y1);
   }
 }
@@ -930,9 +954,9 @@ hipError_t split_cd(const SplitArgs& s, hipStream_t stream) {
   }
 }
 
-template <int DT, int SC, int HALF, int THREADS>
+template <int DT, int SC, int KPARTS, int WORDS, int THREADS>
 hipError_t join_launch(const JoinArgs& j, hipStream_t stream) {
-  hipLaunchKernelGGL((join_kernel<DT, SC, HALF, THREADS>), dim3(j.a.T * j.a.H), dim3(THREADS), 0, stream, j);
+  hipLaunchKernelGGL((join_kernel<DT, SC, KPARTS, WORDS, THREADS>), dim3(j.a.T * j.a.H), dim3(THREADS), 0, stream, j);
   return hipGetLastError();
 }
 
@@ -963,11 +987,11 @@ hipError_t run(const LatentAttnArgs& a, hipStream_t stream) {
   e = split_cd<CD, TQ, TP>(s, stream);
   if (e != hipSuccess) return e;
   JoinArgs j{a, p, s.ml, s.o};
-  // four threads an output, and the words of half a path in registers
+  // two threads an output; high ranks four, a path's words in halves
   const bool wide = a.d_v > 128, high = a.c.r > 256;
-  if (wide)
-    return high ? join_launch<DT, SC, 12, 1024>(j, stream) : join_launch<DT, SC, 4, 1024>(j, stream);
-  return high ? join_launch<DT, SC, 12, 512>(j, stream) : join_launch<DT, SC, 4, 512>(j, stream);
+  if (high)
+    return wide ? join_launch<DT, SC, 2, 12, 1024>(j, stream) : join_launch<DT, SC, 2, 12, 512>(j, stream);
+  return wide ? join_launch<DT, SC, 1, 8, 512>(j, stream) : join_launch<DT, SC, 1, 8, 256>(j, stream);
 }
 template <int DT, int SC>
 hipError_t run_sc(const LatentAttnArgs& a, hipStream_t stream) {
