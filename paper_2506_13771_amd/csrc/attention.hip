@@ -15,7 +15,8 @@ namespace lb {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBM = 128;  // query rows of a workgroup (4 waves x 32)
+constexpr int kWideRows = 128;   // query rows of a workgroup (4 waves x 32)
+constexpr int kSplitKeys = 128;  // keys of a tile that four waves split
 // keys of a step: two tiles of 192 + 128 columns fill half of a CU's LDS (fp32: all of it)
 template <int DT>
 constexpr int keys_of() {
@@ -29,11 +30,16 @@ struct FwdArgs {
   int n_tiles;  // work items per head (an upper bound)
 };
 
-// KC: 16-wide slices of a key's width, VT: 32-wide tiles of a value's.  Two tiles of K
-// and V: the next one's loads run during the products with this one.
-template <int DT, int KC, int VT>
-__global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_fwd(FwdArgs f) {
-  constexpr int KW = 16 * KC, VW = 32 * VT, BN = keys_of<DT>();
+// KC: 16-wide slices of a key's width, VT: 32-wide tiles of a value's.
+// WIDE: a wave has 32 queries of its own and all keys; two tiles of K and V, the next one's
+// loads run during the products with this one.
+// Otherwise the four waves share 32 queries and split the keys, a block of 32 each of one
+// tile, and their sums are joined at the end: a quarter of the steps one after the other,
+// for calls with too few queries and heads to fill the chip with 128-query workgroups.
+template <int DT, int KC, int VT, bool WIDE>
+__global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_fwd(FwdArgs f) {
+  constexpr int KW = 16 * KC, VW = 32 * VT, BN = WIDE ? keys_of<DT>() : kSplitKeys, kBM = WIDE ? kWideRows : 32;
+  constexpr int NB = WIDE ? BN / 32 : 1;  // blocks of 32 keys a wave takes of a tile
   constexpr int KB = tile_bytes<DT, BN, KW>(), TB = KB + tile_bytes<DT, BN, VW>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const AttnArgs& a = f.a;
@@ -53,11 +59,12 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_fwd(FwdAr
   tile = (nq + kBM - 1) / kBM - 1 - tile;
   const int i0 = tile * kBM, off = nk - nq;
   const int dk = a.d_nope + a.d_rope, dv = a.d_v;
-  const int i = i0 + 32 * wave + col;  // this lane's query
+  const int w0 = WIDE ? 32 * wave : 0, rb = WIDE ? 0 : 32 * wave;  // the wave's first query and key in the tiles
+  const int i = i0 + w0 + col;                               // this lane's query
   const int lim = a.causal ? min(nk - 1, i + off) : nk - 1;  // its last key
-  const int lim_lo = a.causal ? min(nk - 1, i0 + 32 * wave + off) : nk - 1;
+  const int lim_lo = a.causal ? min(nk - 1, i0 + w0 + off) : nk - 1;
   const int n_end = a.causal ? min(nk, min(i0 + kBM, nq) + off) : nk;
-  const int w_end = a.causal ? min(n_end, i0 + 32 * wave + 32 + off) : n_end;  // this wave's last key, and one
+  const int w_end = a.causal ? min(n_end, i0 + w0 + 32 + off) : n_end;  // this wave's last key, and one
 
   constexpr int ES = esize<DT>();
   const char* kp = static_cast<const char*>(a.k) + (k_lo * a.k_t + kvh * a.k_h) * ES;
@@ -83,18 +90,28 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_fwd(FwdAr
   const float sc = a.scale * kLog2e;
 
   for (int j0 = 0; j0 < n_end; j0 += BN) {
-    char* kt = smem + (j0 / BN & 1) * TB;
+    char* kt = smem + (WIDE ? (j0 / BN & 1) * TB : 0);
     const char* vt = kt + KB;
-    wait_loads();
-    lds_barrier();  // everyone's loads have arrived, and everyone is done with the other tile
-    if (j0 + BN < n_end) issue(j0 + BN, smem + (~(j0 / BN) & 1) * TB);
-    if (j0 >= w_end) continue;
+    if constexpr (WIDE) {
+      wait_loads();
+      lds_barrier();  // everyone's loads have arrived, and everyone is done with the other tile
+      if (j0 + BN < n_end) issue(j0 + BN, smem + (~(j0 / BN) & 1) * TB);
+    } else {
+      if (j0 > 0) {
+        lds_barrier();
+        issue(j0, smem);
+      }
+      wait_loads();
+      lds_barrier();
+    }
+    const int jw = j0 + rb;  // the wave's first key of the tile
+    if (jw >= w_end) continue;
 
     // S^T: groups of GK fragments, each read while the one before is multiplied
-    constexpr int GK = DT == kDtF32 ? 1 : KC % 4 == 0 ? 4 : 3, NG = BN / 32 * KC / GK;
-    floatx16 s[BN / 32];
+    constexpr int GK = DT == kDtF32 ? 1 : KC % 4 == 0 ? 4 : 3, NG = NB * KC / GK;
+    floatx16 s[NB];
 #pragma unroll
-    for (int b = 0; b < BN / 32; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
     Frag<DT> kf[2][GK];
@@ -104,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_fwd(FwdAr
 #pragma unroll
         for (int n = 0; n < GK; ++n) {
           const int c = (g + 1) * GK + n;
-          kf[(g + 1) & 1][n] = frag_rows<DT, BN>(kt, 32 * (c / KC), 16 * (c % KC), lane);
+          kf[(g + 1) & 1][n] = frag_rows<DT, BN>(kt, rb + 32 * (c / KC), 16 * (c % KC), lane);
         }
       }
       keep_order();
@@ -116,16 +133,16 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_fwd(FwdAr
         }
       }
     }
-    if (j0 + BN - 1 > lim_lo) {
+    if (jw + 32 * NB - 1 > lim_lo) {
 #pragma unroll
-      for (int b = 0; b < BN / 32; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (j0 + 32 * b + 8 * (e >> 2) + 4 * hh + (e & 3) > lim) s[b][e] = -INFINITY;
+          if (jw + 32 * b + 8 * (e >> 2) + 4 * hh + (e & 3) > lim) s[b][e] = -INFINITY;
     }
     float tm = s[0][0];
 #pragma unroll
-    for (int e = 1; e < BN / 2; ++e) tm = fmaxf(tm, s[e >> 4][e & 15]);
+    for (int e = 1; e < 16 * NB; ++e) tm = fmaxf(tm, s[e >> 4][e & 15]);
     tm = fmaxf(tm, __shfl_xor(tm, 32));
     // sums are kept relative to mx, a maximum that follows once it is 2^kSlack behind
     if (__any((tm - mx) * sc > kSlack || (mx == -INFINITY && tm > mx))) {
@@ -142,10 +159,10 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_fwd(FwdAr
     // O^T: slices of 16 keys
     Frag<DT> vf[2][VT];
 #pragma unroll
-    for (int sl = -1; sl < BN / 16; ++sl) {
-      if (sl + 1 < BN / 16) {
+    for (int sl = -1; sl < 2 * NB; ++sl) {
+      if (sl + 1 < 2 * NB) {
 #pragma unroll
-        for (int t = 0; t < VT; ++t) vf[(sl + 1) & 1][t] = frag_cols<DT, BN>(vt, 16 * (sl + 1), 32 * t, lane);
+        for (int t = 0; t < VT; ++t) vf[(sl + 1) & 1][t] = frag_cols<DT, BN>(vt, rb + 16 * (sl + 1), 32 * t, lane);
       }
       keep_order();
       if (sl >= 0) {
@@ -163,31 +180,74 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_fwd(FwdAr
     }
   }
   sum += __shfl_xor(sum, 32);
+  if constexpr (!WIDE) {
+    // the waves' parts of the keys: each wave joins four rows of every accumulator
+    float* part = reinterpret_cast<float*>(smem);  // [wave][VT 16][64]
+    float* stat = part + 4 * VT * 1024;            // [wave][32][2]
+    lds_barrier();
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) part[(wave * VT * 16 + t * 16 + e) * 64 + lane] = o[t][e];
+    if (hh == 0) stat[(wave * 32 + col) * 2] = mx, stat[(wave * 32 + col) * 2 + 1] = sum;
+    lds_barrier();
+    float r[4];
+    mx = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, stat[(w * 32 + col) * 2]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float m = stat[(w * 32 + col) * 2];
+      r[w] = m == -INFINITY ? 0.0f : exp2_fast((m - mx) * sc);
+      sum += r[w] * stat[(w * 32 + col) * 2 + 1];
+    }
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v += r[w] * part[(w * VT * 16 + t * 16 + 4 * wave + q) * 64 + lane];
+        o[t][q] = v;
+      }
+  }
   if (i >= nq) return;
   const float inv = mx == -INFINITY ? 0.0f : 1.0f / sum;
   const int64_t row = static_cast<int64_t>(q_lo + i) * a.H + h;
-  if (a.lse != nullptr && hh == 0) a.lse[row] = mx == -INFINITY ? -INFINITY : mx * a.scale + log2f(sum) * kLn2;
+  if (a.lse != nullptr && hh == 0 && (WIDE || wave == 0))
+    a.lse[row] = mx == -INFINITY ? -INFINITY : mx * a.scale + log2f(sum) * kLn2;
   char* op = static_cast<char*>(a.o) + row * dv * ES;
 #pragma unroll
   for (int t = 0; t < VT; ++t)
 #pragma unroll
-    for (int e = 0; e < 16; e += 4)
-      store4<DT>(op, 32 * t + 2 * e + 4 * hh, dv, f.ovec, o[t][e] * inv, o[t][e + 1] * inv, o[t][e + 2] * inv,
-                 o[t][e + 3] * inv);
+    for (int e = 0; e < (WIDE ? 16 : 4); e += 4)
+      store4<DT>(op, 32 * t + (WIDE ? 2 * e : 8 * wave) + 4 * hh, dv, f.ovec, o[t][e] * inv, o[t][e + 1] * inv,
+                 o[t][e + 2] * inv, o[t][e + 3] * inv);
 }
 
-template <int DT, int KC, int VT>
-hipError_t fwd_launch(const FwdArgs& f, hipStream_t stream) {
+template <int DT, int KC, int VT, bool WIDE>
+hipError_t fwd_launch_form(const FwdArgs& f, hipStream_t stream) {
   static LdsLimit limit;
-  constexpr size_t lds = 2 * static_cast<size_t>(tile_bytes<DT, keys_of<DT>(), 16 * KC + 32 * VT>());
-  const hipError_t e = raise_lds(reinterpret_cast<const void*>(&attn_fwd<DT, KC, VT>), lds, limit);
+  constexpr size_t tiles = WIDE ? 2 * static_cast<size_t>(tile_bytes<DT, keys_of<DT>(), 16 * KC + 32 * VT>())
+                                : static_cast<size_t>(tile_bytes<DT, kSplitKeys, 16 * KC + 32 * VT>());
+  constexpr size_t parts = WIDE ? 0 : 4 * VT * 4096 + 1024;
+  constexpr size_t lds = tiles > parts ? tiles : parts;
+  const hipError_t e = raise_lds(reinterpret_cast<const void*>(&attn_fwd<DT, KC, VT, WIDE>), lds, limit);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attn_fwd<DT, KC, VT>), dim3(static_cast<uint32_t>(f.n_tiles) * f.a.H), dim3(kThreads), lds, stream,
-                     f);
+  hipLaunchKernelGGL((attn_fwd<DT, KC, VT, WIDE>), dim3(static_cast<uint32_t>(f.n_tiles) * f.a.H), dim3(kThreads), lds,
+                     stream, f);
   return hipGetLastError();
 }
+template <int DT, int KC, int VT>
+hipError_t fwd_launch(FwdArgs& f, hipStream_t stream) {
+  const int seqs = f.a.cu_q ? f.a.n_seq : 0;
+  f.n_tiles = (f.a.Tq + kWideRows - 1) / kWideRows + seqs;
+  if (wide_form(f.a.Tq, kWideRows, seqs, f.a.H)) return fwd_launch_form<DT, KC, VT, true>(f, stream);
+  f.n_tiles = (f.a.Tq + 31) / 32 + seqs;
+  return fwd_launch_form<DT, KC, VT, false>(f, stream);
+}
 template <int DT, int VT>
-hipError_t fwd_kc(const FwdArgs& f, hipStream_t stream) {
+hipError_t fwd_kc(FwdArgs& f, hipStream_t stream) {
   const int dk = f.a.d_nope + f.a.d_rope;
   if (dk <= 64) return fwd_launch<DT, 4, VT>(f, stream);
   if (dk <= 96) return fwd_launch<DT, 6, VT>(f, stream);
@@ -195,7 +255,7 @@ hipError_t fwd_kc(const FwdArgs& f, hipStream_t stream) {
   return fwd_launch<DT, 12, VT>(f, stream);
 }
 template <int DT>
-hipError_t fwd_dt(const FwdArgs& f, hipStream_t stream) {
+hipError_t fwd_dt(FwdArgs& f, hipStream_t stream) {
   return f.a.d_v <= 64 ? fwd_kc<DT, 2>(f, stream) : fwd_kc<DT, 4>(f, stream);
 }
 
@@ -216,7 +276,7 @@ bool attn_vec(const AttnArgs& a, bool backward) {
 bool attn_supports(int64_t dk, int64_t dv) { return dk >= 1 && dk <= 192 && dv >= 1 && dv <= 128; }
 
 hipError_t launch_attn_forward(const AttnArgs& a, hipStream_t stream) {
-  FwdArgs f{a, attn_vec(a, false), reinterpret_cast<uintptr_t>(a.o) % 16 == 0 && a.d_v % 4 == 0, (a.Tq + kBM - 1) / kBM + (a.cu_q ? a.n_seq : 0)};
+  FwdArgs f{a, attn_vec(a, false), reinterpret_cast<uintptr_t>(a.o) % 16 == 0 && a.d_v % 4 == 0, 0};
   switch (a.dt) {
     case kDtF32: return fwd_dt<kDtF32>(f, stream);
     case kDtF16: return fwd_dt<kDtF16>(f, stream);

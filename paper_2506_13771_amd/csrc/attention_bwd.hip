@@ -16,13 +16,12 @@ namespace lb {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBM = 128;  // rows a workgroup owns
+constexpr int kWideRows = 128;  // rows a workgroup owns
 
 struct BwdArgs {
   AttnArgs a;
-  int vec;              // rows may be read 16 bytes at a time
+  int vec, ovec;        // rows (those of o) may be read 16 bytes at a time
   int qvec, kvec, vvec;  // dq, dk, dv rows may be written four elements at a time
-  int tiles_q, tiles_k;  // work items per head (upper bounds)
 };
 
 // f16: dS is brought to f16's normal range by a power of two of the largest |dO|
@@ -37,34 +36,15 @@ __device__ __forceinline__ float ds_factor(const float* top) {
   return ldexpf(1.0f, 4 - ex);  // the largest |dO| to [8, 16)
 }
 
-// D, 16 lanes a row; with f16 also the largest |dO| (a maximum: its order does not matter)
-template <int DT>
-__global__ void __launch_bounds__(kThreads) delta_kernel(AttnArgs a, bool vec) {
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads / 16) + threadIdx.x / 16;
-  float s = 0.0f, top = 0.0f;
-  if (row < static_cast<int64_t>(a.Tq) * a.H) {
-    const char* o = static_cast<const char*>(a.o) + row * a.d_v * esize<DT>();
-    const char* d = static_cast<const char*>(a.d_o) + row * a.d_v * esize<DT>();
-    for (int c = 8 * (threadIdx.x & 15); c < a.d_v; c += 128) {
-      const Frag<DT> x = load8<DT>(o, c, a.d_v, vec), y = load8<DT>(d, c, a.d_v, vec);
+// The largest |dO| (f16 only; a maximum: its order does not matter)
+__global__ void __launch_bounds__(kThreads) top_kernel(const uint16_t* d_o, int64_t n, float* top) {
+  float t = 0.0f;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * kThreads)
+    t = fmaxf(t, fabsf(f16_bits_to_f32(d_o[i])));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float v = frag_elem<DT>(y, e);
-        s += frag_elem<DT>(x, e) * v;
-        top = fmaxf(top, fabsf(v));
-      }
-    }
-  }
-#pragma unroll
-  for (int m = 8; m > 0; m >>= 1) s += __shfl_xor(s, m);
-  if ((threadIdx.x & 15) == 0 && row < static_cast<int64_t>(a.Tq) * a.H) a.delta[row] = s;
-  if constexpr (DT == kDtF16) {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-    if ((threadIdx.x & 63) == 0 && top > 0.0f)
-      __hip_atomic_fetch_max(reinterpret_cast<uint32_t*>(a.top), __float_as_uint(top), __ATOMIC_RELAXED,
-                             __HIP_MEMORY_SCOPE_AGENT);
-  }
+  for (int m = 32; m > 0; m >>= 1) t = fmaxf(t, __shfl_xor(t, m));
+  if ((threadIdx.x & 63) == 0 && t > 0.0f)
+    __hip_atomic_fetch_max(reinterpret_cast<uint32_t*>(top), __float_as_uint(t), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // S and dO V^T of a 32 x 32 block: A operands from rows of the tiles t0 (KC slices) and
@@ -133,20 +113,43 @@ __device__ __forceinline__ void add_products(const char* tile, int row0, int lan
   }
 }
 
-// rows of a step: two tiles of 192 + 128 columns fill half of a CU's LDS
-template <int DT>
-constexpr int step_of() {
-  return DT == kDtF32 ? 32 : 64;
+// Four waves' parts of an accumulator added, in their order: wave w gets rows 8 w + 4 (lane /
+// 32) + q of its column in v[q].  buf: 16 KB.
+__device__ __forceinline__ void join_waves(float* buf, const floatx16& x, int wave, int lane, float (&v)[4]) {
+  lds_barrier();
+#pragma unroll
+  for (int e = 0; e < 16; ++e) buf[(wave * 16 + e) * 64 + lane] = x[e];
+  lds_barrier();
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    v[q] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v[q] += buf[(w * 16 + 4 * wave + q) * 64 + lane];
+  }
 }
+
+// rows of a step: two tiles of 192 + 128 columns fill half of a CU's LDS; one tile that
+// four waves split (32 rows each) where they share the workgroup's rows
+template <int DT, bool WIDE>
+constexpr int step_of() {
+  return !WIDE ? 128 : DT == kDtF32 ? 32 : 64;
+}
+template <int DT, int KC, int VT, bool WIDE>
+constexpr size_t lds_of(bool stats) {  // stats: 8 bytes a row (the keys' kernel)
+  constexpr int B = step_of<DT, WIDE>();
+  return (WIDE ? 2 : 1) * static_cast<size_t>(tile_bytes<DT, B, 16 * KC + 32 * VT>() + (stats ? 8 * B : 0));
+}
+constexpr size_t kLdsMax = 163840;
 
 // queries: dQ.  For queries with few keys D is formed anew as sum_j P (dO V^T): the one
 // from the rounded O is off by up to half a step of it, which where few keys share the
 // weight is as large as the rounding of dS and the result together (at 20 keys 1.6 times
 // the result's own rounding, at 600 1.1 times).
 constexpr int kExactKeys = 512;
-template <int DT, int KC, int VT>
-__global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_bwd_queries(BwdArgs f) {
-  constexpr int BN = step_of<DT>(), KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
+// WIDE and its other form: as in the forward.
+template <int DT, int KC, int VT, bool WIDE>
+__global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_bwd_queries(BwdArgs f) {
+  constexpr int BN = step_of<DT, WIDE>(), kBM = WIDE ? kWideRows : 32, NB = WIDE ? BN / 32 : 1, KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
   constexpr int SG = DT == kDtF32 ? 1 : KC > 8 ? 2 : 4;  // fragments read ahead: two waves a SIMD leave 256 registers
   constexpr int KB = tile_bytes<DT, BN, KW>(), TB = KB + tile_bytes<DT, BN, VW>(), ES = esize<DT>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -163,12 +166,13 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_bwd_queri
   seq_range(a.cu_k, seq, a.Tk, k_lo, k_hi);
   const int nq = q_hi - q_lo, nk = k_hi - k_lo, off = nk - nq;
   tile = (nq + kBM - 1) / kBM - 1 - tile;  // the longest first
-  const int i0 = tile * kBM, i = i0 + 32 * wave + col;
+  const int w0 = WIDE ? 32 * wave : 0, rb = WIDE ? 0 : 32 * wave;  // the wave's first query and key in the tiles
+  const int i0 = tile * kBM, i = i0 + w0 + col;
   const int dk = a.d_nope + a.d_rope, dv = a.d_v;
   const int lim = a.causal ? min(nk - 1, i + off) : nk - 1;
-  const int lim_lo = a.causal ? min(nk - 1, i0 + 32 * wave + off) : nk - 1;
+  const int lim_lo = a.causal ? min(nk - 1, i0 + w0 + off) : nk - 1;
   const int n_end = a.causal ? min(nk, min(i0 + kBM, nq) + off) : nk;
-  const int w_end = a.causal ? min(n_end, i0 + 32 * wave + 32 + off) : n_end;
+  const int w_end = a.causal ? min(n_end, i0 + w0 + 32 + off) : n_end;
   const float sc = a.scale * kLog2e;
   const float fac = ds_factor<DT>(a.top);
 
@@ -192,8 +196,19 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_bwd_queri
     for (int c = 0; c < 2 * VT; ++c) df[c] = load8<DT>(dp, 16 * c + 8 * hh, dv, f.vec);
   }
   const float l = a.lse[row];
-  float del = a.delta[row];
   const float l2 = l == -INFINITY ? INFINITY : l * kLog2e;
+  // D of the given O: in the row's two lanes, half of the columns each
+  float del = 0.0f;
+  {
+    const char* op = static_cast<const char*>(a.o) + row * dv * ES;
+#pragma unroll
+    for (int c = 0; c < 2 * VT; ++c) {
+      const Frag<DT> x = load8<DT>(op, 16 * c + 8 * hh, dv, f.ovec);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) del += frag_elem<DT>(x, e) * frag_elem<DT>(df[c], e);
+    }
+    del += __shfl_xor(del, 32);
+  }
   // P in s, from S; the mask where the block reaches past a query's last key
   auto probabilities = [&](int j, floatx16& s) {
     const bool mask = j + 31 > lim_lo;
@@ -203,21 +218,31 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_bwd_queri
       if (mask && j + 8 * (e >> 2) + 4 * hh + (e & 3) > lim) s[e] = 0.0f;
     }
   };
-  int at = 0;  // the tile that is read
+  int at = 0;  // the tile that is read (the other form: whether it has been read)
   // the keys' tiles in turn; the last step issues the first tile again if `more`
   auto walk = [&](bool more, auto&& block) {
     for (int j0 = 0; j0 < n_end; j0 += BN) {
-      char* kt = smem + at * TB;
-      at ^= 1;
-      wait_loads();
-      lds_barrier();
-      if (j0 + BN < n_end)
-        issue(j0 + BN, smem + at * TB);
-      else if (more)
-        issue(0, smem + at * TB);
-      if (j0 >= w_end) continue;
+      char* kt = smem + (WIDE ? at * TB : 0);
+      if constexpr (WIDE) {
+        at ^= 1;
+        wait_loads();
+        lds_barrier();
+        if (j0 + BN < n_end)
+          issue(j0 + BN, smem + at * TB);
+        else if (more)
+          issue(0, smem + at * TB);
+      } else {
+        if (at > 0) {
+          lds_barrier();
+          issue(j0, smem);
+        }
+        at = 1;
+        wait_loads();
+        lds_barrier();
+      }
+      if (j0 + rb >= w_end) continue;
 #pragma unroll
-      for (int b = 0; b < BN / 32; ++b) block(kt, kt + KB, 32 * b, j0 + 32 * b);
+      for (int b = 0; b < NB; ++b) block(kt, kt + KB, rb + 32 * b, j0 + rb + 32 * b);
     }
   };
   if (n_end <= kExactKeys) {
@@ -230,8 +255,15 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_bwd_queri
       for (int e = 0; e < 16; ++e) d += s[e] == 0.0f ? 0.0f : s[e] * dp[e];
     });
     del = d + __shfl_xor(d, 32);
-    if (hh == 0 && i < nq) a.delta[row] = del;  // (read by the keys' kernel, which runs after this one)
+    if constexpr (!WIDE) {
+      float* part = reinterpret_cast<float*>(smem);
+      lds_barrier();
+      if (hh == 0) part[wave * 32 + col] = del;
+      lds_barrier();
+      del = (part[col] + part[32 + col]) + (part[64 + col] + part[96 + col]);
+    }
   }
+  if (hh == 0 && i < nq && (WIDE || wave == 0)) a.delta[row] = del;  // (read by the keys' kernel, which runs after this one)
   floatx16 gq[KT];
 #pragma unroll
   for (int t = 0; t < KT; ++t)
@@ -245,21 +277,30 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 ? 1 : 2) attn_bwd_queri
     for (int e = 0; e < 16; ++e) dp[e] = s[e] == 0.0f ? 0.0f : s[e] * (dp[e] - del) * fac;
     add_products<DT, KT, BN, SG>(kt, r0, lane, dp, gq);
   });
-  if (i >= nq) return;
   const float qs = a.scale / fac;
   char* gp = static_cast<char*>(a.dq) + row * dk * ES;
 #pragma unroll
-  for (int n = 0; n < KT; ++n)
+  for (int n = 0; n < KT; ++n) {
+    if constexpr (WIDE) {
+      if (i < nq) {
 #pragma unroll
-    for (int e = 0; e < 16; e += 4)
-      store4<DT>(gp, 32 * n + 2 * e + 4 * hh, dk, f.qvec, gq[n][e] * qs, gq[n][e + 1] * qs, gq[n][e + 2] * qs,
-                 gq[n][e + 3] * qs);
+        for (int e = 0; e < 16; e += 4)
+          store4<DT>(gp, 32 * n + 2 * e + 4 * hh, dk, f.qvec, gq[n][e] * qs, gq[n][e + 1] * qs, gq[n][e + 2] * qs,
+                     gq[n][e + 3] * qs);
+      }
+    } else {
+      float v[4];
+      join_waves(reinterpret_cast<float*>(smem), gq[n], wave, lane, v);
+      if (i < nq) store4<DT>(gp, 32 * n + 8 * wave + 4 * hh, dk, f.qvec, v[0] * qs, v[1] * qs, v[2] * qs, v[3] * qs);
+    }
+  }
 }
 
 // keys: dK, dV
-template <int DT, int KC, int VT>
+// Not WIDE: the four waves share 32 keys and split the queries.
+template <int DT, int KC, int VT, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
-  constexpr int BQ = step_of<DT>(), KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
+  constexpr int BQ = step_of<DT, WIDE>(), kBM = WIDE ? kWideRows : 32, NB = WIDE ? BQ / 32 : 1, KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
   constexpr int KB = tile_bytes<DT, BQ, KW>(), TB = KB + tile_bytes<DT, BQ, VW>() + 8 * BQ, ES = esize<DT>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const AttnArgs& a = f.a;
@@ -273,7 +314,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
   seq_range(a.cu_q, seq, a.Tq, q_lo, q_hi);
   seq_range(a.cu_k, seq, a.Tk, k_lo, k_hi);
   const int nq = q_hi - q_lo, nk = k_hi - k_lo, off = nk - nq;
-  const int j0 = tile * kBM, j = j0 + 32 * wave + col;  // this lane's key
+  const int w0 = WIDE ? 32 * wave : 0, rb = WIDE ? 0 : 32 * wave;  // the wave's first key and query in the tiles
+  const int j0 = tile * kBM, j = j0 + w0 + col;                    // this lane's key
   const int dk = a.d_nope + a.d_rope, dv = a.d_v;
   const float sc = a.scale * kLog2e;
   const float fac = ds_factor<DT>(a.top);
@@ -339,34 +381,41 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) gv[t][e] = 0.0f;
 
-  int i_now = i_begin;
+  int i_now = i_begin, g_now = 0;
   for (int it = 0; it < total; ++it) {
-    const char* qt = smem + (it & 1) * TB;
+    char* qt = smem + (WIDE ? (it & 1) * TB : 0);
     const char* dt = qt + KB;
     const float* st = reinterpret_cast<const float*>(qt + TB - 8 * BQ);
+    if (!WIDE && it > 0) {
+      lds_barrier();
+      put_stats(i_now, qt);  // (this step's: fetched during the one before)
+      fetch_stats(i1, g1);
+      issue(i_now, g_now, qt);
+    }
     wait_loads();
     lds_barrier();
-    const int i_here = i_now;
-    i_now = i1;
+    const int i_here = i_now + rb;
+    i_now = i1, g_now = g1;
     if (it + 1 < total) {
-      char* t = smem + (~it & 1) * TB;
-      put_stats(i1, t);
-      const int ii = i1, gi = g1;
       next(i1, g1);
-      fetch_stats(i1, g1);
-      issue(ii, gi, t);
+      if constexpr (WIDE) {
+        char* t = smem + (~it & 1) * TB;
+        put_stats(i_now, t);
+        fetch_stats(i1, g1);
+        issue(i_now, g_now, t);
+      }
     }
-    if (a.causal && i_here + BQ - 1 + off < j0 + 32 * wave) continue;  // every query before the wave's first key
+    if (a.causal && i_here + 32 * NB - 1 + off < j0 + w0) continue;  // every query before the wave's first key
 #pragma unroll
-    for (int b = 0; b < BQ / 32; ++b) {
+    for (int b = 0; b < NB; ++b) {
       floatx16 s, dp;
-      scores<DT, KC, 2 * VT, BQ>(qt, dt, 32 * b, lane, kf, vf, s, dp);
-      const bool mask = a.causal && i_here + 32 * b + off < j0 + 32 * wave + 31;
+      scores<DT, KC, 2 * VT, BQ>(qt, dt, rb + 32 * b, lane, kf, vf, s, dp);
+      const bool mask = a.causal && i_here + 32 * b + off < j0 + w0 + 31;
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
         const int row = 32 * b + 2 * e + 4 * hh;
-        const float4 l4 = *reinterpret_cast<const float4*>(st + row);
-        const float4 d4 = *reinterpret_cast<const float4*>(st + BQ + row);
+        const float4 l4 = *reinterpret_cast<const float4*>(st + rb + row);
+        const float4 d4 = *reinterpret_cast<const float4*>(st + BQ + rb + row);
         const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -376,31 +425,49 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
           dp[e + q] = p == 0.0f ? 0.0f : p * (dp[e + q] - dl[q]) * fac;
         }
       }
-      add_products<DT, VT, BQ>(dt, 32 * b, lane, s, gv);
-      add_products<DT, KT, BQ>(qt, 32 * b, lane, dp, gk);
+      add_products<DT, VT, BQ>(dt, rb + 32 * b, lane, s, gv);
+      add_products<DT, KT, BQ>(qt, rb + 32 * b, lane, dp, gk);
     }
   }
-  if (j >= nk) return;
-  const int64_t t = k_lo + j;
+  const int64_t t = k_lo + min(j, nk - 1);
   const float ks = a.scale / fac;
   char* gkp = static_cast<char*>(a.dk) + (t * a.dk_t + kvh * a.dk_h) * ES;
   char* gvp = static_cast<char*>(a.dv) + (t * a.dv_t + kvh * a.dv_h) * ES;
   float* grp = a.dkr_part + (static_cast<int64_t>(kvh) * a.Tk + t) * a.d_rope;
+  auto put_v = [&](int c, float v0, float v1, float v2, float v3) {
+    if (j < nk) store4<DT>(gvp, c, dv, f.vvec, v0, v1, v2, v3);
+  };
+  auto put_k = [&](int c, float v0, float v1, float v2, float v3) {
+    if (j >= nk) return;
+    const float v[4] = {v0 * ks, v1 * ks, v2 * ks, v3 * ks};
+    store4<DT>(gkp, c, a.d_nope, f.kvec, v[0], v[1], v[2], v[3]);
 #pragma unroll
-  for (int n = 0; n < VT; ++n)
+    for (int q = 0; q < 4; ++q)
+      if (c + q >= a.d_nope && c + q < dk) grp[c + q - a.d_nope] = v[q];
+  };
+  float* buf = reinterpret_cast<float*>(smem);
 #pragma unroll
-    for (int e = 0; e < 16; e += 4)
-      store4<DT>(gvp, 32 * n + 2 * e + 4 * hh, dv, f.vvec, gv[n][e], gv[n][e + 1], gv[n][e + 2], gv[n][e + 3]);
+  for (int n = 0; n < VT; ++n) {
+    if constexpr (WIDE) {
 #pragma unroll
-  for (int n = 0; n < KT; ++n)
-#pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-      const int c = 32 * n + 2 * e + 4 * hh;
-      store4<DT>(gkp, c, a.d_nope, f.kvec, gk[n][e] * ks, gk[n][e + 1] * ks, gk[n][e + 2] * ks, gk[n][e + 3] * ks);
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (c + q >= a.d_nope && c + q < dk) grp[c + q - a.d_nope] = gk[n][e + q] * ks;
+      for (int e = 0; e < 16; e += 4) put_v(32 * n + 2 * e + 4 * hh, gv[n][e], gv[n][e + 1], gv[n][e + 2], gv[n][e + 3]);
+    } else {
+      float v[4];
+      join_waves(buf, gv[n], wave, lane, v);
+      put_v(32 * n + 8 * wave + 4 * hh, v[0], v[1], v[2], v[3]);
     }
+  }
+#pragma unroll
+  for (int n = 0; n < KT; ++n) {
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) put_k(32 * n + 2 * e + 4 * hh, gk[n][e], gk[n][e + 1], gk[n][e + 2], gk[n][e + 3]);
+    } else {
+      float v[4];
+      join_waves(buf, gk[n], wave, lane, v);
+      put_k(32 * n + 8 * wave + 4 * hh, v[0], v[1], v[2], v[3]);
+    }
+  }
 }
 
 // the shared rotary key's gradient: the key heads' partial results in order
@@ -417,27 +484,40 @@ __global__ void __launch_bounds__(kThreads) rope_sum(AttnArgs a) {
   st<DT>(a.dkr, n, s);
 }
 
+// one of the two kernels in the form that fits the call
+template <int DT, int KC, int VT, bool QUERIES, bool WIDE>
+hipError_t bwd_one(const BwdArgs& f, int T, const int32_t* cu, int heads, hipStream_t stream) {
+  constexpr size_t lds = lds_of<DT, KC, VT, WIDE>(!QUERIES);
+  constexpr int rows = WIDE ? kWideRows : 32;
+  const dim3 grid(static_cast<uint32_t>((T + rows - 1) / rows + (cu ? f.a.n_seq : 0)) * heads);
+  static LdsLimit limit;
+  if constexpr (QUERIES) {
+    const hipError_t e = raise_lds(reinterpret_cast<const void*>(&attn_bwd_queries<DT, KC, VT, WIDE>), lds, limit);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((attn_bwd_queries<DT, KC, VT, WIDE>), grid, dim3(kThreads), lds, stream, f);
+  } else {
+    const hipError_t e = raise_lds(reinterpret_cast<const void*>(&attn_bwd_keys<DT, KC, VT, WIDE>), lds, limit);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((attn_bwd_keys<DT, KC, VT, WIDE>), grid, dim3(kThreads), lds, stream, f);
+  }
+  return hipGetLastError();
+}
+template <int DT, int KC, int VT, bool QUERIES>
+hipError_t bwd_form(const BwdArgs& f, int T, const int32_t* cu, int heads, hipStream_t stream) {
+  if (T == 0) return hipSuccess;
+  // (the widest fp32 heads' 128 rows do not fit)
+  if constexpr (lds_of<DT, KC, VT, false>(!QUERIES) <= kLdsMax) {
+    if (!wide_form(T, kWideRows, cu ? f.a.n_seq : 0, heads))
+      return bwd_one<DT, KC, VT, QUERIES, false>(f, T, cu, heads, stream);
+  }
+  return bwd_one<DT, KC, VT, QUERIES, true>(f, T, cu, heads, stream);
+}
 template <int DT, int KC, int VT>
 hipError_t bwd_launch(const BwdArgs& f, hipStream_t stream) {
-  constexpr int B = step_of<DT>();
-  constexpr size_t tiles = 2 * static_cast<size_t>(tile_bytes<DT, B, 16 * KC + 32 * VT>()), stats = 2 * 8 * B;
-  static LdsLimit lk, lq;
-  hipError_t e = raise_lds(reinterpret_cast<const void*>(&attn_bwd_keys<DT, KC, VT>), tiles + stats, lk);
+  hipError_t e = bwd_form<DT, KC, VT, true>(f, f.a.Tq, f.a.cu_q, f.a.H, stream);
   if (e != hipSuccess) return e;
-  e = raise_lds(reinterpret_cast<const void*>(&attn_bwd_queries<DT, KC, VT>), tiles, lq);
+  e = bwd_form<DT, KC, VT, false>(f, f.a.Tk, f.a.cu_k, f.a.Hk, stream);
   if (e != hipSuccess) return e;
-  if (f.tiles_q > 0) {
-    hipLaunchKernelGGL((attn_bwd_queries<DT, KC, VT>), dim3(static_cast<uint32_t>(f.tiles_q) * f.a.H), dim3(kThreads),
-                       tiles, stream, f);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (f.tiles_k > 0) {
-    hipLaunchKernelGGL((attn_bwd_keys<DT, KC, VT>), dim3(static_cast<uint32_t>(f.tiles_k) * f.a.Hk), dim3(kThreads),
-                       tiles + stats, stream, f);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   if (f.a.d_rope > 0 && f.a.Tk > 0) {
     const int64_t n = static_cast<int64_t>(f.a.Tk) * f.a.d_rope;
     hipLaunchKernelGGL((rope_sum<DT>), dim3(static_cast<uint32_t>((n + kThreads - 1) / kThreads)), dim3(kThreads), 0,
@@ -457,16 +537,16 @@ template <int DT>
 hipError_t bwd_dt(const BwdArgs& f, hipStream_t stream) {
   const AttnArgs& a = f.a;
   if constexpr (DT == kDtF16) {
-    const hipError_t e = launch_zero_elems(a.top, 1, kDtF32, stream);
+    hipError_t e = launch_zero_elems(a.top, 1, kDtF32, stream);
     if (e != hipSuccess) return e;
-  }
-  if (a.Tq > 0) {
-    const bool vec = f.vec && reinterpret_cast<uintptr_t>(a.o) % 16 == 0;
-    const int64_t rows = static_cast<int64_t>(a.Tq) * a.H;
-    hipLaunchKernelGGL((delta_kernel<DT>), dim3(static_cast<uint32_t>((rows + 15) / 16)), dim3(kThreads), 0, stream, a,
-                       vec);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    const int64_t n = static_cast<int64_t>(a.Tq) * a.H * a.d_v;
+    if (n > 0) {
+      const int64_t blocks = (n + 8 * kThreads - 1) / (8 * kThreads);
+      hipLaunchKernelGGL(top_kernel, dim3(static_cast<uint32_t>(blocks < 2048 ? blocks : 2048)), dim3(kThreads), 0, stream,
+                         static_cast<const uint16_t*>(a.d_o), n, a.top);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   }
   return a.d_v <= 64 ? bwd_kc<DT, 2>(f, stream) : bwd_kc<DT, 4>(f, stream);
 }
@@ -483,8 +563,7 @@ hipError_t launch_attn_backward(const AttnArgs& a, hipStream_t stream) {
   f.qvec = ok(a.dq, 0, 0, a.d_nope + a.d_rope);
   f.kvec = ok(a.dk, a.dk_t, a.dk_h, a.d_nope);
   f.vvec = ok(a.dv, a.dv_t, a.dv_h, a.d_v);
-  f.tiles_q = a.Tq == 0 ? 0 : (a.Tq + kBM - 1) / kBM + (a.cu_q ? a.n_seq : 0);
-  f.tiles_k = a.Tk == 0 ? 0 : (a.Tk + kBM - 1) / kBM + (a.cu_k ? a.n_seq : 0);
+  f.ovec = f.vec && reinterpret_cast<uintptr_t>(a.o) % 16 == 0;
   switch (a.dt) {
     case kDtF32: return bwd_dt<kDtF32>(f, stream);
     case kDtF16: return bwd_dt<kDtF16>(f, stream);

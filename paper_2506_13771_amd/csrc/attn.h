@@ -76,6 +76,13 @@ struct AttnArgs {
   float* dkr_part;  // [Hk][Tk][d_rope]
 };
 
+// Whether workgroups of 128 rows (a wave 32 of them) do for T rows in n_seq sequences and
+// `heads` heads: they fill half of the 256 CUs or more, half a workgroup counted for each
+// sequence's last.  Otherwise a workgroup's waves split the other axis of 32 rows.
+inline bool wide_form(int64_t T, int rows, int n_seq, int64_t heads) {
+  return (T / rows + (n_seq + 1) / 2) * heads >= 128;
+}
+
 hipError_t launch_rotate(const RotateArgs& a, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, hipStream_t stream);
 size_t latent_attn_workspace_bytes(int T, int n_seq, int H, int r, int d_rope);
