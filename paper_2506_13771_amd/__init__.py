@@ -608,15 +608,13 @@ def lb_rotate(x, positions, freqs, inverse: bool = False, out=None, stream=None)
     (i, i + d / 2); inverse=True turns back, which is also the gradient's map.  x and out may be strided
     (last dimension contiguous), out may be x; returns out."""
     torch = _torch()
-    if x.dim() != 3:
-        raise ValueError("x must be [T, H, d]")
     shape = x.shape
+    T, H, d = shape
     if out is None:
         out = x.new_empty(shape)
     else:
         _need(out, shape, x.dtype, "out")
     _on_gpu(x, positions, freqs, out)
-    T, H, d = shape
     px, sx = _rows(x, "x")
     py, sy = _rows(out, "out")
     st = load_library().lb_rotate(px, _dtype_code(x), T, H, d, sx[0], sx[1], _whole(positions, (T,), torch.int32, "positions"),

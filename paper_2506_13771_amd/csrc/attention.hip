@@ -242,7 +242,10 @@ template <int DT, int KC, int VT>
 hipError_t fwd_launch(FwdArgs& f, hipStream_t stream) {
   const int seqs = f.a.cu_q ? f.a.n_seq : 0;
   f.n_tiles = (f.a.Tq + kWideRows - 1) / kWideRows + seqs;
-  if (wide_form(f.a.Tq, kWideRows, seqs, f.a.H)) return fwd_launch_form<DT, KC, VT, true>(f, stream);
+  // us, this form against the other (7B heads, bf16): 96 workgroups (256 rows) 13.1 against 10.8, 160
+  // (512) 20.8 against 23.1, 192 (4 x 512) 9.9 against 16.0; fp32, 64 wide: 72 91.9 against 34.2, 136
+  // 182 against 79
+  if (wide_groups(f.a.Tq, seqs, f.a.H) >= (DT == kDtF32 ? 400 : 128)) return fwd_launch_form<DT, KC, VT, true>(f, stream);
   f.n_tiles = (f.a.Tq + 31) / 32 + seqs;
   return fwd_launch_form<DT, KC, VT, false>(f, stream);
 }

@@ -505,9 +505,13 @@ hipError_t bwd_one(const BwdArgs& f, int T, const int32_t* cu, int heads, hipStr
 template <int DT, int KC, int VT, bool QUERIES>
 hipError_t bwd_form(const BwdArgs& f, int T, const int32_t* cu, int heads, hipStream_t stream) {
   if (T == 0) return hipSuccess;
-  // (the widest fp32 heads' 128 rows do not fit)
+  // us of the whole backward with this form of the queries' kernel, and of the keys', against the
+  // other (7B heads, bf16): 160 workgroups (512 rows) 85 against 70, 91 against 85; 192 (4 x 512) 51 against
+  // 51, 49 against 51; 224 (768) 109 against 107, 103 against 109; 288 (1024) 141 against 154, 118 against
+  // 141; fp32, 64 wide, 136 (2048): 360 against 223, 543 against 360.  Four queries' heads a key head: 136
+  // 422 against 257 for the keys.  (The widest fp32 heads' 128 rows do not fit.)
   if constexpr (lds_of<DT, KC, VT, false>(!QUERIES) <= kLdsMax) {
-    if (!wide_form(T, kWideRows, cu ? f.a.n_seq : 0, heads))
+    if (wide_groups(T, cu ? f.a.n_seq : 0, heads) < (DT == kDtF32 ? 400 : 210))
       return bwd_one<DT, KC, VT, QUERIES, false>(f, T, cu, heads, stream);
   }
   return bwd_one<DT, KC, VT, QUERIES, true>(f, T, cu, heads, stream);

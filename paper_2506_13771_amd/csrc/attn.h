@@ -76,12 +76,10 @@ struct AttnArgs {
   float* dkr_part;  // [Hk][Tk][d_rope]
 };
 
-// Whether workgroups of 128 rows (a wave 32 of them) do for T rows in n_seq sequences and
-// `heads` heads: they fill half of the 256 CUs or more, half a workgroup counted for each
-// sequence's last.  Otherwise a workgroup's waves split the other axis of 32 rows.
-inline bool wide_form(int64_t T, int rows, int n_seq, int64_t heads) {
-  return (T / rows + (n_seq + 1) / 2) * heads >= 128;
-}
+// The number of 128-row workgroups (a wave 32 of the rows) that T rows of n_seq sequences and
+// `heads` heads make, half of one counted for each sequence's last.  Below a kernel's
+// limit the other form runs: 32 rows a workgroup, whose waves split the other axis.
+inline int64_t wide_groups(int64_t T, int n_seq, int64_t heads) { return (T / 128 + (n_seq + 1) / 2) * heads; }
 
 hipError_t launch_rotate(const RotateArgs& a, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, hipStream_t stream);

@@ -342,13 +342,13 @@ EXPANDED = [  # lens_q, lens_k, H, Hk, dn, dr, dv, causal, dtype
     ([300], [257], 2, 2, 0, 64, 128, False, "f32"),                # the rotary key alone
     ([128, 256], [128, 256], 8, 1, 64, 64, 128, True, "f16"),      # one key head
     # enough heads for workgroups of 128 rows
-    ([200, 130], [200, 130], 64, 64, 64, 0, 64, True, "bf16"),
-    ([150, 1, 70], [200, 5, 70], 64, 64, 128, 64, 128, True, "bf16"),
-    ([260, 0, 33], [140, 9, 33], 64, 64, 64, 32, 128, True, "f16"),
-    ([129, 100], [129, 100], 64, 64, 33, 7, 56, False, "f32"),
-    ([190], [190], 128, 64, 96, 16, 40, True, "f16"),
-    ([140, 140], [300, 140], 64, 64, 128, 0, 128, True, "f32"),
-    ([130, 64], [130, 64], 64, 64, 120, 64, 128, False, "f32"),
+    ([200, 230], [200, 230], 64, 64, 64, 0, 64, True, "bf16"),
+    ([150, 1, 170], [200, 5, 170], 64, 64, 128, 64, 128, True, "bf16"),
+    ([260, 0, 33], [240, 9, 33], 64, 64, 64, 32, 128, True, "f16"),
+    ([129, 100], [129, 100], 192, 192, 33, 7, 56, False, "f32"),
+    ([290], [290], 128, 64, 96, 16, 40, True, "f16"),
+    ([140, 140], [150, 140], 144, 144, 128, 0, 128, True, "f32"),
+    ([130, 64], [130, 64], 208, 208, 120, 64, 128, False, "f32"),
 ]
 
 
