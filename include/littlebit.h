@@ -476,7 +476,7 @@ lb_status lb_dual_svid(const void* W, lb_dtype w_dtype, int64_t d_out, int64_t d
    and not seen; rows behind cu[n_seq] are neither read nor written.  A place
    named twice in one append holds parts of either token.
    2 r + d_rope <= 1536, d_rope even and <= 256, n_pages page_size < 2^31 and
-   max_pages page_size < 2^31 (LB_ERR_SHAPE); data may be larger than 2^31
+   max_pages page_size <= 2^30 (LB_ERR_SHAPE); data may be larger than 2^31
    elements and is 16-byte aligned. */
 typedef struct lb_latent_cache {
   void* data;
@@ -523,7 +523,7 @@ lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const vo
    query's position (freqs; NULL: taken as they are); out [T x H x d_v]
    contiguous, in act_dtype.  A query that sees no token gets 0.  Only U and h of
    the paths are read (of the fused layer, d_out = Hk (d_nope + d_v)).  H a
-   multiple of Hk; d_nope, d_v <= 256; (T H / 32 + n_seq) (max_pages page_size / 16
+   multiple of Hk; d_nope, d_v <= 256; T H < 2^22; (T H / 32 + n_seq) (max_pages page_size / 16
    + 1) < 2^31 (LB_ERR_SHAPE); scale finite and > 0
    (LB_ERR_ARG).  q' enters the scores with at least 16 significant bits (24 for
    fp32 activations), softmax statistics and sums are fp32; probabilities enter
@@ -547,8 +547,9 @@ lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int6
    cu_q, cu_k [n_seq + 1] int32: prefix sums of the sequences' queries and keys,
    both NULL for one sequence of all rows.  causal != 0: query i of n_q sees keys
    j <= i + n_k - n_q of its sequence.  Query head h reads key head h / (H / Hk).
-   1 <= d_nope + d_rope <= 192, 1 <= d_v <= 128 (LB_ERR_SHAPE); scale finite and
-   > 0 (LB_ERR_ARG).  Rows behind cu_q[n_seq] / cu_k[n_seq] are neither read nor
+   1 <= d_nope + d_rope <= 192, 1 <= d_v <= 128, (Tq / 128 + n_seq + 1) H and (Tk /
+   128 + n_seq + 1) Hk < 2^24 (LB_ERR_SHAPE); scale finite and > 0 (LB_ERR_ARG).
+   Rows behind cu_q[n_seq] / cu_k[n_seq] are neither read nor
    written; accesses stay inside the buffers whatever cu_q and cu_k hold.  A
    masked score is left out whatever its key holds, but a NaN or infinity in v may
    reach queries of its sequence that do not see it (a zero probability is

@@ -20,6 +20,7 @@ The names follow the C ABI:
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import struct
@@ -578,6 +579,15 @@ def _on_gpu(*tensors):
             raise ValueError(f"every tensor must be on the current GPU (cuda:{cur}), got one on {t.device}")
 
 
+_NO_CONTEXT = contextlib.nullcontext()
+
+
+def _memory_of(stream):
+    """Where a call's new tensors are allocated: with the stream that it runs on, so that their memory is not
+    handed on while that stream still uses it."""
+    return _NO_CONTEXT if stream is None else _torch().cuda.stream(stream)
+
+
 def _need(t, shape, dtype, name: str):
     if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
@@ -611,7 +621,8 @@ def lb_rotate(x, positions, freqs, inverse: bool = False, out=None, stream=None)
     shape = x.shape
     T, H, d = shape
     if out is None:
-        out = x.new_empty(shape)
+        with _memory_of(stream):
+            out = x.new_empty(shape)
     else:
         _need(out, shape, x.dtype, "out")
     _on_gpu(x, positions, freqs, out)
@@ -708,10 +719,11 @@ def lb_latent_attention(q, cache: LatentCache, paths: Sequence[LittleBitPath], H
     sdt = a.h.dtype
     arr = _PACK_PATHS(a.U.data_ptr(), 0, _whole(a.h, (n_out,), sdt, "h"), 0, 0,
                       b.U.data_ptr(), 0, _whole(b.h, (n_out,), sdt, "h"), 0, 0)
-    if out is None:
-        out = q.new_empty((T, H, d_v))
-    if workspace is None:
-        workspace = _scratch(lb_latent_attention_workspace_bytes(T, lens.shape[0], H, r, dr), q.device)
+    with _memory_of(stream):
+        if out is None:
+            out = q.new_empty((T, H, d_v))
+        if workspace is None:
+            workspace = _scratch(lb_latent_attention_workspace_bytes(T, lens.shape[0], H, r, dr), q.device)
     pq, sq = _rows(q, "q")
     st = load_library().lb_latent_attention(
         pq, _dtype_code(q), T, H, Hk, dn, d_v, sq[0], sq[1], arr, _dtype_code(a.h), cache._packed(table, lens, cu),
@@ -764,10 +776,11 @@ def lb_attention_forward(q, k, v, k_rope=None, cu_q=None, cu_k=None, causal: boo
     torch = _torch()
     _on_gpu(q, k, v, k_rope, cu_q, cu_k, o, lse)
     a, (Tq, _, H, _, _, _, d_v) = _packed_attention(q, k, v, k_rope, cu_q, cu_k, causal, scale)
-    if o is None:
-        o = q.new_empty((Tq, H, d_v))
-    if lse is None:
-        lse = q.new_empty((Tq, H), dtype=torch.float32)
+    with _memory_of(stream):
+        if o is None:
+            o = q.new_empty((Tq, H, d_v))
+        if lse is None:
+            lse = q.new_empty((Tq, H), dtype=torch.float32)
     st = load_library().lb_attention_forward(a, _whole(o, (Tq, H, d_v), q.dtype, "o"),
                                              _whole(lse, (Tq, H), torch.float32, "lse"), _stream(stream))
     if st:
@@ -787,24 +800,20 @@ def lb_attention_backward(q, k, v, k_rope, o, lse, d_o, cu_q=None, cu_k=None, ca
     _on_gpu(q, k, v, k_rope, o, lse, d_o, cu_q, cu_k, dq, dk, dv, dk_rope, workspace)
     a, (Tq, Tk, H, Hk, dn, dr, d_v) = _packed_attention(q, k, v, k_rope, cu_q, cu_k, causal, scale)
     dt = q.dtype
-    dq = q.new_empty((Tq, H, dn + dr)) if dq is None else dq
-    if dk is None:
-        dk = q.new_empty((Tk, Hk, dn))
-    else:
-        _need(dk, (Tk, Hk, dn), dt, "dk")
-    if dv is None:
-        dv = q.new_empty((Tk, Hk, d_v))
-    else:
-        _need(dv, (Tk, Hk, d_v), dt, "dv")
-    pr = 0
-    if dr:
-        dk_rope = q.new_empty((Tk, dr)) if dk_rope is None else dk_rope
-        pr = _whole(dk_rope, (Tk, dr), dt, "dk_rope")
+    with _memory_of(stream):
+        dq = q.new_empty((Tq, H, dn + dr)) if dq is None else dq
+        dk = q.new_empty((Tk, Hk, dn)) if dk is None else dk
+        dv = q.new_empty((Tk, Hk, d_v)) if dv is None else dv
+        if dr and dk_rope is None:
+            dk_rope = q.new_empty((Tk, dr))
+        if workspace is None:
+            workspace = _scratch(lb_attention_backward_workspace_bytes(Tq, Tk, H, Hk, dr), q.device)
+    _need(dk, (Tk, Hk, dn), dt, "dk")
+    _need(dv, (Tk, Hk, d_v), dt, "dv")
+    pr = _whole(dk_rope, (Tk, dr), dt, "dk_rope") if dr else 0
     pk, sk = _rows(dk, "dk")
     pv, sv = _rows(dv, "dv")
     g = _PACK_GRADS(_whole(dq, (Tq, H, dn + dr), dt, "dq"), pk, pv, pr, sk[0], sk[1], sv[0], sv[1])
-    if workspace is None:
-        workspace = _scratch(lb_attention_backward_workspace_bytes(Tq, Tk, H, Hk, dr), q.device)
     st = load_library().lb_attention_backward(
         a, _whole(o, (Tq, H, d_v), dt, "o"), _whole(lse, (Tq, H), torch.float32, "lse"),
         _whole(d_o, (Tq, H, d_v), dt, "d_o"), g, _dev_ptr(workspace, "workspace"),

@@ -23,6 +23,10 @@ bool dtype_ok(const lb_dtype& d) {
 int64_t dtype_size(lb_dtype d) { return d == LB_F32 ? 4 : 2; }
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
+// a launch's threads are counted in 32 bits: rows (token, head) with a workgroup of up to
+// 1024 threads each, and workgroups of 256
+constexpr int64_t kMaxRows = int64_t(1) << 22, kMaxGroups = int64_t(1) << 24;
+
 // a b (and a b c) below 2^31, all factors >= 0
 bool fits(int64_t a, int64_t b) { return a == 0 || b <= kMaxElems / a; }
 bool fits(int64_t a, int64_t b, int64_t c) { return fits(a, b) && fits(a * b, c); }
@@ -54,7 +58,7 @@ lb_status check_cache(const lb_latent_cache* c) {
   if (!dtype_ok(c->dtype)) return LB_ERR_DTYPE;
   if (!cache_sizes_ok(c->r, c->d_rope) || c->n_pages < 0 || c->page_size < 1 || c->n_seq < 0 || c->max_pages < 0 ||
       c->n_seq > (1 << 24) || !fits(c->n_pages, c->page_size) || !fits(c->max_pages, c->page_size) ||
-      !fits(c->n_seq, c->max_pages))
+      c->max_pages * c->page_size > (1 << 30) || !fits(c->n_seq, c->max_pages))
     return LB_ERR_SHAPE;
   return LB_OK;
 }
@@ -160,7 +164,7 @@ lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int6
   if (st != LB_OK) return st;
   if (T < 0 || H < 0 || Hk < 1 || H % Hk != 0 || d_nope < 0 || d_nope > 256 || d_v < 0 || d_v > 256 ||
       !strides_ok(q_t, q_h) || !fits(T, H, lb::latent_row(cache->r, cache->d_rope)) ||
-      !fits(T, H, d_nope + cache->d_rope) || !fits(T, H, d_v) || !fits(Hk, d_nope + d_v, cache->r))
+      !fits(T, H, d_nope + cache->d_rope) || !fits(T, H, d_v) || !fits(Hk, d_nope + d_v, cache->r) || T * H >= kMaxRows)
     return LB_ERR_SHAPE;
   // the kernels count steps of 16 tokens or more of items of 32 query rows in 31 bits
   if (!fits(T * H / 32 + cache->n_seq, cache->max_pages * cache->page_size / 16 + 1)) return LB_ERR_SHAPE;
@@ -176,7 +180,10 @@ lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int6
   }
   st = check_cache_ptrs(cache);
   if (st != LB_OK) return st;
-  if (ranges_meet(out, T * H * d_v * es, q, span(T, H, d_nope + cache->d_rope, q_t, q_h) * es)) return LB_ERR_ARG;
+  const int64_t no = T * H * d_v * es;
+  const int64_t nc = cache->n_pages * cache->page_size * lb::latent_row(cache->r, cache->d_rope) * dtype_size(cache->dtype);
+  if (ranges_meet(out, no, q, span(T, H, d_nope + cache->d_rope, q_t, q_h) * es) || ranges_meet(out, no, cache->data, nc))
+    return LB_ERR_ARG;
   const size_t need = lb_latent_attention_workspace_bytes(T, cache->n_seq, H, cache->r, cache->d_rope);
   if (!workspace) return LB_ERR_NULL;
   if (!aligned(workspace, 256)) return LB_ERR_ALIGN;
@@ -211,7 +218,8 @@ lb_status check_attention(const lb_attention* a) {
     return LB_ERR_SHAPE;
   const int64_t dk = a->d_nope + a->d_rope;
   if (!fits(a->Tq, a->H, dk) || !fits(a->Tq, a->H, a->d_v) || !fits(a->Tk, a->Hk, dk) || !fits(a->Tk, a->Hk, a->d_v) ||
-      !fits(a->n_seq + 1, a->H))
+      !fits(a->n_seq + 1, a->H) || (a->Tq / 128 + a->n_seq + 1) * a->H >= kMaxGroups ||
+      (a->Tk / 128 + a->n_seq + 1) * a->Hk >= kMaxGroups)
     return LB_ERR_SHAPE;
   if ((a->cu_q == nullptr) != (a->cu_k == nullptr) || !scale_ok(a->scale)) return LB_ERR_ARG;
   return LB_OK;

@@ -80,7 +80,7 @@ hipError_t rotate_dt(const RotateArgs& a, hipStream_t stream) {
   constexpr int VP = 16 / esize<DT>();
   const int half = a.d / 2;
   auto ok = [&](const void* p, int64_t st, int64_t sh) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && st % VP == 0 && sh % VP == 0;
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (a.T == 1 || st % VP == 0) && (a.H == 1 || sh % VP == 0);
   };
   const bool vec = half % VP == 0 && ok(a.x, a.x_t, a.x_h) && ok(a.y, a.y_t, a.y_h);
   const int niv = vec ? half / VP : half, nhg = (a.H + kRHeads - 1) / kRHeads;

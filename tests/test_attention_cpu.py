@@ -68,7 +68,7 @@ def _cache(**kw):
 CACHES = [
     (dict(dtype=9), DTYPE), (dict(n_pages=-1), SHAPE), (dict(page_size=0), SHAPE), (dict(r=0), SHAPE), (dict(r=769), SHAPE),
     (dict(d_rope=7), SHAPE), (dict(d_rope=258), SHAPE), (dict(r=768, d_rope=2), SHAPE), (dict(n_seq=-1), SHAPE),
-    (dict(max_pages=-1), SHAPE), (dict(n_pages=1 << 27, page_size=16), SHAPE), (dict(max_pages=1 << 30, page_size=2), SHAPE),
+    (dict(max_pages=-1), SHAPE), (dict(n_pages=1 << 27, page_size=16), SHAPE), (dict(max_pages=1 << 30, page_size=2), SHAPE), (dict(max_pages=(1 << 30) + 1, page_size=1, n_seq=1), SHAPE),
     (dict(data=0), NULL), (dict(table=0), NULL), (dict(lens=0), NULL), (dict(cu=0), NULL), (dict(data=P + 8), ALIGN),
     (dict(table=P + 2), ALIGN), (dict(cu=P + 1), ALIGN)]
 
@@ -121,7 +121,8 @@ def test_latent_attention_refuses_caches(lib, kw, want):
     (dict(scale=float("nan")), ARG), (dict(scale=float("inf")), ARG), (dict(q=0), NULL), (dict(out=0), NULL),
     (dict(ws=0), NULL), (dict(paths=_paths(U=0)), NULL), (dict(paths=_paths(h=0)), NULL), (dict(paths=_paths(U=P + 2)), ALIGN),
     (dict(paths=_paths(h=P + 1)), ALIGN), (dict(q=64 * P + 1), ALIGN), (dict(out=128 * P + 1), ALIGN),
-    (dict(ws=256 * P + 128), ALIGN), (dict(n=1000), WORKSPACE), (dict(out=64 * P + 320), ARG), (dict(T=0), OK),
+    (dict(ws=256 * P + 128), ALIGN), (dict(n=1000), WORKSPACE), (dict(out=64 * P + 320), ARG), (dict(out=P + 64), ARG),
+    (dict(T=1 << 20, cache=_cache(r=1, d_rope=0), dn=1, dv=1), SHAPE), (dict(T=0), OK),
     (dict(dv=0), OK), (dict(cache=_cache(n_seq=0)), OK)])
 def test_latent_attention_refuses(lib, kw, want):
     assert _latent(lib, **kw) == want
@@ -138,7 +139,7 @@ ATTNS = [
     (dict(dtype=7), DTYPE), (dict(Tq=-1), SHAPE), (dict(Tk=-1), SHAPE), (dict(H=5), SHAPE), (dict(Hk=0), SHAPE),
     (dict(d_nope=0, d_rope=0), SHAPE), (dict(d_nope=180, d_rope=13), SHAPE), (dict(d_nope=-8, d_rope=24), SHAPE),
     (dict(d_v=0), SHAPE), (dict(d_v=129), SHAPE), (dict(n_seq=-1), SHAPE), (dict(q_t=-1), SHAPE), (dict(v_h=-1), SHAPE),
-    (dict(Tq=1 << 30), SHAPE), (dict(cu_q=P), ARG), (dict(cu_k=P), ARG), (dict(scale=0.0), ARG),
+    (dict(Tq=1 << 30), SHAPE), (dict(cu_q=P, cu_k=P, n_seq=1 << 22), SHAPE), (dict(cu_q=P), ARG), (dict(cu_k=P), ARG), (dict(scale=0.0), ARG),
     (dict(scale=float("nan")), ARG), (dict(q=0), NULL), (dict(k=0), NULL), (dict(v=0), NULL), (dict(k_rope=0), NULL),
     (dict(q=P + 1), ALIGN), (dict(k=16 * P + 1), ALIGN), (dict(v=32 * P + 1), ALIGN), (dict(k_rope=48 * P + 1), ALIGN),
     (dict(cu_q=P + 1, cu_k=P, n_seq=1), ALIGN)]

@@ -341,6 +341,7 @@ EXPANDED = [  # lens_q, lens_k, H, Hk, dn, dr, dv, causal, dtype
     ([50, 40], [50, 60], 2, 2, 21, 0, 128, True, "bf16"),
     ([300], [257], 2, 2, 0, 64, 128, False, "f32"),                # the rotary key alone
     ([128, 256], [128, 256], 8, 1, 64, 64, 128, True, "f16"),      # one key head
+    ([60, 9], [60, 300], 2, 2, 128, 64, 128, True, "f32"),         # the widest fp32 heads
     # enough heads for workgroups of 128 rows
     ([200, 230], [200, 230], 64, 64, 64, 0, 64, True, "bf16"),
     ([150, 1, 170], [200, 5, 170], 64, 64, 128, 64, 128, True, "bf16"),
