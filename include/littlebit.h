@@ -528,7 +528,9 @@ lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const vo
    (LB_ERR_ARG).  q' enters the scores with at least 16 significant bits (24 for
    fp32 activations), softmax statistics and sums are fp32; probabilities enter
    the sums rounded to the cache's type where out's is no finer, else in two or
-   three terms of it (22 bits or more for fp32 activations).
+   three terms of it (22 bits or more for fp32 activations).  A NaN or infinity in
+   the row of a new token may reach the call's earlier queries of its sequence,
+   which do not see it (a zero probability is multiplied with it).
    workspace: 256-byte aligned, >= lb_latent_attention_workspace_bytes(T, n_seq,
    H, r, d_rope) bytes (0 for invalid sizes), no zero-fill needed; calls that may
    run concurrently need distinct workspaces.  Repeated calls give the same bits. */
