@@ -40,6 +40,7 @@ template <int DT, int KC, int VT, bool WIDE>
 __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_fwd(FwdArgs f) {
   constexpr int KW = 16 * KC, VW = 32 * VT, BN = WIDE ? keys_of<DT>() : kSplitKeys, kBM = WIDE ? kWideRows : 32;
   constexpr int NB = WIDE ? BN / 32 : 1;  // blocks of 32 keys a wave takes of a tile
+  constexpr bool SPREAD = WIDE && DT != kDtF32;  // the next tile's loads one at a time (rows fit 16-byte loads)
   constexpr int KB = tile_bytes<DT, BN, KW>(), TB = KB + tile_bytes<DT, BN, VW>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const AttnArgs& a = f.a;
@@ -75,6 +76,16 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
                                     nk - j0, f.vec, tid);
     tile_load<DT, BN, VW, kThreads>(t + KB, vp + j0 * a.v_t * ES, a.v_t, dv, nullptr, 0, 0, nk - j0, f.vec, tid);
   };
+  TileLoads<DT, SPREAD ? BN : 64, KW, kThreads> kl;
+  TileLoads<DT, SPREAD ? BN : 64, VW, kThreads> vl;
+  auto tick = [&](int n) {
+    if constexpr (SPREAD) {
+      if (n < kl.LOADS)
+        kl.load(n);
+      else if (n < kl.LOADS + vl.LOADS)
+        vl.load(n - kl.LOADS);
+    }
+  };
   if (n_end > 0) issue(0, smem);
   const char* qp = static_cast<const char*>(a.q) + ((q_lo + min(i, nq - 1)) * a.q_t + h * a.q_h) * ES;
   Frag<DT> qf[KC];
@@ -95,7 +106,15 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
     if constexpr (WIDE) {
       wait_loads();
       lds_barrier();  // everyone's loads have arrived, and everyone is done with the other tile
-      if (j0 + BN < n_end) issue(j0 + BN, smem + (~(j0 / BN) & 1) * TB);
+      char* to = smem + (~(j0 / BN) & 1) * TB;
+      if constexpr (SPREAD) {
+        // (after the last tile, itself again: no branch between the products)
+        const int jn = j0 + BN < n_end ? j0 + BN : j0;
+        kl.start(to, kp + jn * a.k_t * ES, a.k_t, a.d_nope, rp + jn * a.kr_t * ES, a.kr_t, a.d_rope, nk - jn, tid);
+        vl.start(to + KB, vp + jn * a.v_t * ES, a.v_t, dv, nullptr, 0, 0, nk - jn, tid);
+      } else if (j0 + BN < n_end) {
+        issue(j0 + BN, to);
+      }
     } else {
       if (j0 > 0) {
         lds_barrier();
@@ -105,10 +124,14 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
       lds_barrier();
     }
     const int jw = j0 + rb;  // the wave's first key of the tile
-    if (jw >= w_end) continue;
+    if (jw >= w_end) {
+#pragma unroll
+      for (int n = 0; n < kl.LOADS + vl.LOADS; ++n) tick(n);
+      continue;
+    }
 
     // S^T: groups of GK fragments, each read while the one before is multiplied
-    constexpr int GK = DT == kDtF32 ? 1 : KC % 4 == 0 ? 4 : 3, NG = NB * KC / GK;
+    constexpr int GK = DT == kDtF32 ? 1 : 4, NG = NB * KC / GK;
     floatx16 s[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -126,6 +149,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
       }
       keep_order();
       if (g >= 0) {
+        tick(g);
 #pragma unroll
         for (int n = 0; n < GK; ++n) {
           const int c = g * GK + n;
@@ -166,6 +190,11 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
       }
       keep_order();
       if (sl >= 0) {
+        if (sl + 1 < 2 * NB)
+          tick(NG + sl);
+        else  // the rest
+#pragma unroll
+          for (int n = NG + sl; n < kl.LOADS + vl.LOADS; ++n) tick(n);
         // the probabilities in the operands' type: one rounding each (their sum keeps 32 bits)
         float pv[8];
 #pragma unroll
@@ -179,6 +208,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
       }
     }
   }
+  if constexpr (SPREAD) wait_loads();  // none may arrive after the workgroup's end
   sum += __shfl_xor(sum, 32);
   if constexpr (!WIDE) {
     // the waves' parts of the keys: each wave joins four rows of every accumulator
@@ -242,10 +272,11 @@ template <int DT, int KC, int VT>
 hipError_t fwd_launch(FwdArgs& f, hipStream_t stream) {
   const int seqs = f.a.cu_q ? f.a.n_seq : 0;
   f.n_tiles = (f.a.Tq + kWideRows - 1) / kWideRows + seqs;
+  // (16-bit rows that fit no 16-byte loads take the other form, whose loads go through registers.)
   // us, this form against the other (7B heads, bf16): 96 workgroups (256 rows) 13.1 against 10.8, 160
   // (512) 20.8 against 23.1, 192 (4 x 512) 9.9 against 16.0; fp32, 64 wide: 72 91.9 against 34.2, 136
   // 182 against 79
-  if (wide_groups(f.a.Tq, seqs, f.a.H) >= (DT == kDtF32 ? 400 : 128)) return fwd_launch_form<DT, KC, VT, true>(f, stream);
+  if (wide_groups(f.a.Tq, seqs, f.a.H) >= (DT == kDtF32 ? 400 : 128) && (f.vec || DT == kDtF32)) return fwd_launch_form<DT, KC, VT, true>(f, stream);
   f.n_tiles = (f.a.Tq + 31) / 32 + seqs;
   return fwd_launch_form<DT, KC, VT, false>(f, stream);
 }
@@ -253,7 +284,6 @@ template <int DT, int VT>
 hipError_t fwd_kc(FwdArgs& f, hipStream_t stream) {
   const int dk = f.a.d_nope + f.a.d_rope;
   if (dk <= 64) return fwd_launch<DT, 4, VT>(f, stream);
-  if (dk <= 96) return fwd_launch<DT, 6, VT>(f, stream);
   if (dk <= 128) return fwd_launch<DT, 8, VT>(f, stream);
   return fwd_launch<DT, 12, VT>(f, stream);
 }

@@ -443,12 +443,19 @@ struct SplitArgs {
   float* o;
 };
 
-// An LDS tile holds its tokens' columns of one wave, unit by unit (attn_common.h).
+// An LDS tile holds its tokens' columns of one wave, unit by unit: a unit's rows of PU
+// 16-byte pieces (4; fp32: 8), piece q of row t at q ^ unit_swz(t).  Row-wise reads (16
+// rows at one piece) then meet 16 different slots of the 64 banks, transposed reads
+// (8 rows of 4 pieces) each slot twice, the least.
+template <int CD>
+__device__ __forceinline__ int unit_swz(int t) {
+  return CD == kDtF32 ? (t >> 1) & 7 : (t >> 2) & 3;
+}
 // row lane % tpt of a unit at columns 16 half + 8 (lane / 32) ..
 template <int CD>
 __device__ __forceinline__ Frag<CD> tile_rows(const char* unit, int tpt, int half, int lane) {
   constexpr int PU = 2 * esize<CD>();
-  const int t = lane & (tpt - 1), s = swz<CD>(t);
+  const int t = lane & (tpt - 1), s = unit_swz<CD>(t);
   const char* p = unit + t * PU * 16;
   Frag<CD> f;
   if constexpr (CD == kDtF32) {
@@ -472,14 +479,14 @@ __device__ __forceinline__ Frag<CD> tile_cols(const char* t, int s, int lane) {
     for (int k = 0; k < 8; ++k) {
       const int row = 16 * s + 8 * (k >> 2) + 4 * hh + (k & 3);
       f.v[k >> 2][k & 3] =
-          *reinterpret_cast<const uint32_t*>(t + row * PU * 16 + 16 * (q ^ swz<CD>(row)) + 4 * (lane & 3));
+          *reinterpret_cast<const uint32_t*>(t + row * PU * 16 + 16 * (q ^ unit_swz<CD>(row)) + 4 * (lane & 3));
     }
   } else {
     typedef __attribute__((address_space(3))) s16x4* lds4;
     const int i = lane & 15, q = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
     const int row = 16 * s + 4 * hh + (i >> 2);
-    const char* p0 = t + row * PU * 16 + 16 * (q ^ swz<CD>(row)) + 8 * (i & 1);
-    const char* p1 = t + (row + 8) * PU * 16 + 16 * (q ^ swz<CD>(row + 8)) + 8 * (i & 1);
+    const char* p0 = t + row * PU * 16 + 16 * (q ^ unit_swz<CD>(row)) + 8 * (i & 1);
+    const char* p1 = t + (row + 8) * PU * 16 + 16 * (q ^ unit_swz<CD>(row + 8)) + 8 * (i & 1);
     const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0)));
     const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1)));
     f.v[0] = u32x4{a[0], a[1], b[0], b[1]};
@@ -553,7 +560,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
 #pragma unroll
       for (int n = 0; n < NL; ++n) {
         const int t = lane / PU + n * TPL;
-        src[n] = data + __shfl(idx, t & (p.tpt - 1)) * row_bytes + 16 * ((lane & (PU - 1)) ^ swz<CD>(t));
+        src[n] = data + __shfl(idx, t & (p.tpt - 1)) * row_bytes + 16 * ((lane & (PU - 1)) ^ unit_swz<CD>(t));
       }
 #pragma unroll
       for (int u = 0; u < UPW; ++u) {
