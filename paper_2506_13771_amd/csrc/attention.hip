@@ -76,8 +76,9 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
                                     nk - j0, f.vec, tid);
     tile_load<DT, BN, VW, kThreads>(t + KB, vp + j0 * a.v_t * ES, a.v_t, dv, nullptr, 0, 0, nk - j0, f.vec, tid);
   };
-  TileLoads<DT, SPREAD ? BN : 64, KW, kThreads> kl;
-  TileLoads<DT, SPREAD ? BN : 64, VW, kThreads> vl;
+  constexpr int R4 = 256 / pieces<DT>();  // (BN where SPREAD)
+  TileLoads<DT, R4, KW, kThreads> kl;
+  TileLoads<DT, R4, VW, kThreads> vl;
   auto tick = [&](int n) {
     if constexpr (SPREAD) {
       if (n < kl.LOADS)

@@ -166,34 +166,33 @@ __device__ __forceinline__ void store4(void* row, int col, int n, bool vec, floa
 }
 
 // ---------------------------------------------------------------------------
-// LDS tiles of R rows, by units of 128 bytes a row (64 columns; fp32: 32): [unit][row][8
-// pieces of 16 bytes], piece q of row t at q ^ swz(t).  Row-wise reads (16 rows at one
-// piece) then meet 16 different slots of the 64 banks and transposed 16-bit reads (8 rows of
-// 4 pieces) each slot twice, the least; and a load from memory into LDS (64 lanes' pieces
-// in a row) takes whole cache lines of 8 rows.  (No bank conflicts counted in any of the
-// kernels; units of 64 bytes, 16 rows a load, take as long.)
+// LDS tiles of R rows, by units of 32 columns: [unit][row][pieces of 16 bytes], PU pieces
+// a row (4; fp32: 8), piece q of row t at q ^ swz(t).  Row-wise reads (16 rows at one
+// piece) then meet 16 different slots of the 64 banks and transposed reads (8 rows of 4
+// pieces) each slot twice, the least; and a load from memory into LDS (64 lanes' pieces
+// in a row) takes the same pieces of 64 / PU rows in every unit.  (No bank conflicts counted
+// in any kernel.  16-bit units of 64 columns, 8 rows a load, load no faster and their reads
+// need twice the addresses: keys' gradient 330 -> 355 us.)
 // ---------------------------------------------------------------------------
+
 template <int DT>
-constexpr int unit_cols() {
-  return 128 / esize<DT>();
+constexpr int pieces() {
+  return 2 * esize<DT>();
 }
 template <int DT>
 __device__ __forceinline__ int swz(int t) {
-  const int s = (t >> 1) & 7;
-  // 16 bits: the low bit first exchanged between the halves of a unit that transposed reads take
-  return DT == kDtF32 ? s : ((s & 1) << 2) | (s & 2) | (s >> 2);
+  return DT == kDtF32 ? (t >> 1) & 7 : (t >> 2) & 3;
 }
 template <int DT, int R, int W>
 constexpr int tile_bytes() {
-  static_assert(W % unit_cols<DT>() == 0, "whole units");
   return R * W * esize<DT>();
 }
 // eight elements at row t, columns col .. col + 7
 template <int DT, int R>
 __device__ __forceinline__ void tile_put(char* tile, int t, int col, const Frag<DT>& f) {
-  constexpr int UC = unit_cols<DT>();
-  char* p = tile + (col / UC * R + t) * 128;
-  const int q = col % UC * esize<DT>() / 16, s = swz<DT>(t);
+  constexpr int PU = pieces<DT>();
+  char* p = tile + ((col >> 5) * R + t) * PU * 16;
+  const int q = (col & 31) * esize<DT>() / 16, s = swz<DT>(t);
   *reinterpret_cast<u32x4*>(p + 16 * (q ^ s)) = f.v[0];
   if constexpr (DT == kDtF32) *reinterpret_cast<u32x4*>(p + 16 * ((q + 1) ^ s)) = f.v[1];
 }
@@ -201,13 +200,19 @@ __device__ __forceinline__ void tile_put(char* tile, int t, int col, const Frag<
 // (row0 a multiple of 32, col of 16)
 template <int DT, int R>
 __device__ __forceinline__ Frag<DT> frag_rows(const char* tile, int row0, int col, int lane) {
-  constexpr int UC = unit_cols<DT>();
+  constexpr int PU = pieces<DT>();
   const int t = lane & 31, s = swz<DT>(t);
-  const char* p = tile + t * 128;
-  const int o = (col / UC * R + row0) * 128, q = (col % UC + 8 * (lane >> 5)) * esize<DT>() / 16;
+  const char* p = tile + t * PU * 16;
+  const int o = ((col >> 5) * R + row0) * PU * 16;
   Frag<DT> f;
-  f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * (q ^ s) + o);
-  if constexpr (DT == kDtF32) f.v[1] = *reinterpret_cast<const u32x4*>(p + 16 * ((q + 1) ^ s) + o);
+  if constexpr (DT == kDtF32) {
+    const int q = 4 * ((col >> 4) & 1) + 2 * (lane >> 5);
+    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * (q ^ s) + o);
+    f.v[1] = *reinterpret_cast<const u32x4*>(p + 16 * ((q + 1) ^ s) + o);
+  } else {
+    const int q = 2 * ((col >> 4) & 1) + (lane >> 5);
+    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * (q ^ s) + o);
+  }
   return f;
 }
 // A operand from columns: lane l takes column col + l % 32 at rows row0 + 8 a + 4 (l / 32)
@@ -215,21 +220,22 @@ __device__ __forceinline__ Frag<DT> frag_rows(const char* tile, int row0, int co
 // reads (each 16-lane group takes 4 rows x 16 columns).
 template <int DT, int R>
 __device__ __forceinline__ Frag<DT> frag_cols(const char* tile, int row0, int col, int lane) {
-  constexpr int UC = unit_cols<DT>();
-  const int u = lane >> 5, o = (col / UC * R + row0) * 128;
+  constexpr int PU = pieces<DT>();
+  const int u = lane >> 5, o = ((col >> 5) * R + row0) * PU * 16;
   Frag<DT> f;
   if constexpr (DT == kDtF32) {
     const int q = (lane & 31) >> 2;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int t = 8 * (k >> 2) + 4 * u + (k & 3);  // (16 rows on, swz is the same)
-      f.v[k >> 2][k & 3] = *reinterpret_cast<const uint32_t*>(tile + t * 128 + 16 * (q ^ swz<DT>(t)) + 4 * (lane & 3) + o);
+      f.v[k >> 2][k & 3] =
+          *reinterpret_cast<const uint32_t*>(tile + t * PU * 16 + 16 * (q ^ swz<DT>(t)) + 4 * (lane & 3) + o);
     }
   } else {
     typedef __attribute__((address_space(3))) s16x4* lds4;
-    const int i = lane & 15, q = col % UC / 8 + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1), t = 4 * u + (i >> 2);
-    const char* p0 = tile + t * 128 + 16 * (q ^ swz<DT>(t)) + 8 * (i & 1);
-    const char* p1 = tile + (t + 8) * 128 + 16 * (q ^ swz<DT>(t + 8)) + 8 * (i & 1);
+    const int i = lane & 15, q = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1), t = 4 * u + (i >> 2);
+    const char* p0 = tile + t * PU * 16 + 16 * (q ^ swz<DT>(t)) + 8 * (i & 1);
+    const char* p1 = tile + (t + 8) * PU * 16 + 16 * (q ^ swz<DT>(t + 8)) + 8 * (i & 1);
     const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0 + o)));
     const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1 + o)));
     f.v[0] = u32x4{a[0], a[1], b[0], b[1]};
@@ -262,23 +268,23 @@ __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x
 template <int DT, int R, int W, int THREADS>
 __device__ __forceinline__ void tile_load(char* tile, const char* p0, int64_t s0, int n0, const char* p1, int64_t s1, int n1,
                                           int n_rows, bool vec, int tid) {
-  constexpr int ES = esize<DT>(), UC = unit_cols<DT>(), NW = THREADS / 64;
+  constexpr int ES = esize<DT>(), PU = pieces<DT>(), TPL = 64 / PU, NW = THREADS / 64;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (vec) {
-    static_assert(R / 8 % NW == 0, "whole rounds of the waves");
+    static_assert(R / TPL % NW == 0, "whole rounds of the waves");
 #pragma unroll
-    for (int g = 0; g < R / 8; g += NW) {
-      const int gw = g + wave, t = gw * 8 + lane / 8;
-      const int c = ((lane & 7) ^ swz<DT>(t)) * (16 / ES);  // column within the unit
+    for (int g = 0; g < R / TPL; g += NW) {
+      const int gw = g + wave, t = gw * TPL + lane / PU;
+      const int c = ((lane & (PU - 1)) ^ swz<DT>(t)) * (16 / ES);  // column within the unit
       const int64_t row = min(t, n_rows - 1);
       const char* a = p0 + row * s0 * ES + c * ES;
       const char* b = n1 > 0 ? p1 + row * s1 * ES + (c - n0) * ES : a;
 #pragma unroll
-      for (int u = 0; u < W / UC; ++u) {
-        const int col = UC * u + c;
-        const char* src = (col < n0 ? a : b) + u * 128;
-        if (UC * (u + 1) > n0 + n1) src = col < n0 + n1 ? src : reinterpret_cast<const char*>(kZeros);
-        load_lds16(src, tile + (u * R + gw * 8) * 128);
+      for (int u = 0; u < W / 32; ++u) {
+        const int col = 32 * u + c;
+        const char* src = (col < n0 ? a : b) + u * 32 * ES;
+        src = col < n0 + n1 ? src : reinterpret_cast<const char*>(kZeros);
+        load_lds16(src, tile + (u * R + gw * TPL) * PU * 16);
       }
     }
   } else {
@@ -292,36 +298,31 @@ __device__ __forceinline__ void tile_load(char* tile, const char* p0, int64_t s0
 
 // The loads of such a tile one at a time (n = 0 .. LOADS - 1, known at compile time), so that they
 // stand between products: all at once, a wave waits some 2000 cycles for the queue to take its ten.
-// (Forward of 2 x 2048 tokens of 7B heads: 148 -> 128 us.  Their addresses take 16 registers, which the
-// backward's kernels do not have: they load all at once.)
+// (Forward of 2 x 2048 tokens of 7B heads: 148 -> 130 us.)
 template <int DT, int R, int W, int THREADS>
 struct TileLoads {
-  static constexpr int UNITS = W / unit_cols<DT>(), ROUNDS = R / 8 / (THREADS / 64), LOADS = UNITS * ROUNDS;
-  const char *a[ROUNDS], *b[ROUNDS];
-  int c, n0, n, wave;
+  static constexpr int PU = pieces<DT>(), TPL = 64 / PU, LOADS = W / 32;
+  static_assert(R == TPL * (THREADS / 64), "one round of the waves");
+  const char *a, *b;
+  int c, n0, n;
   char* tile;
   __device__ __forceinline__ void start(char* to, const char* p0, int64_t s0, int w0, const char* p1, int64_t s1, int w1,
                                         int n_rows, int tid) {
-    constexpr int ES = esize<DT>(), NW = THREADS / 64;
-    const int lane = tid & 63;
-    wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    tile = to, n0 = w0, n = w0 + w1;
-    c = ((lane & 7) ^ swz<DT>(wave * 8 + lane / 8)) * (16 / ES);
-#pragma unroll
-    for (int g = 0; g < ROUNDS; ++g) {
-      // (NW rounds of 8 rows on, swz is the same: R / ROUNDS is a multiple of 16)
-      static_assert(8 * NW % 16 == 0, "rows of a round");
-      const int64_t row = min((g * NW + wave) * 8 + lane / 8, n_rows - 1);
-      a[g] = p0 + row * s0 * ES + c * ES;
-      b[g] = w1 > 0 ? p1 + row * s1 * ES + (c - w0) * ES : a[g];
-    }
+    constexpr int ES = esize<DT>();
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), t = wave * TPL + lane / PU;
+    n0 = w0, n = w0 + w1;
+    c = ((lane & (PU - 1)) ^ swz<DT>(t)) * (16 / ES);
+    const int64_t row = min(t, n_rows - 1);
+    a = p0 + row * s0 * ES + c * ES;
+    b = w1 > 0 ? p1 + row * s1 * ES + (c - w0) * ES : a;
+    tile = to + wave * TPL * PU * 16;
   }
-  __device__ __forceinline__ void load(int i) const {
-    constexpr int UC = unit_cols<DT>(), NW = THREADS / 64;
-    const int u = i % UNITS, g = i / UNITS, col = UC * u + c;
-    const char* src = (col < n0 ? a[g] : b[g]) + u * 128;
+  __device__ __forceinline__ void load(int u) const {
+    constexpr int ES = esize<DT>();
+    const int col = 32 * u + c;
+    const char* src = (col < n0 ? a : b) + u * 32 * ES;
     src = col < n ? src : reinterpret_cast<const char*>(kZeros);
-    load_lds16(src, tile + (u * R + (g * NW + wave) * 8) * 128);
+    load_lds16(src, tile + u * R * PU * 16);
   }
 };
 
