@@ -49,10 +49,10 @@ __global__ void __launch_bounds__(kThreads) top_kernel(const uint16_t* d_o, int6
 
 // S and dO V^T of a 32 x 32 block: A operands from rows of the tiles t0 (KC slices) and
 // t1 (2 VT slices), B operands in registers; groups of GK fragments, each read while the
-// one before is multiplied.
-template <int DT, int KC, int VC, int R, int GK = (DT == kDtF32 ? 1 : 4)>
+// one before is multiplied; tick(g) stands before group g's products.
+template <int DT, int KC, int VC, int R, int GK, typename TICK>
 __device__ __forceinline__ void scores(const char* t0, const char* t1, int row0, int lane, const Frag<DT> (&b0)[KC],
-                                       const Frag<DT> (&b1)[VC], floatx16& s, floatx16& dp) {
+                                       const Frag<DT> (&b1)[VC], floatx16& s, floatx16& dp, TICK&& tick) {
   constexpr int N = KC + VC, NG = (N + GK - 1) / GK;
 #pragma unroll
   for (int e = 0; e < 16; ++e) s[e] = 0.0f, dp[e] = 0.0f;
@@ -69,6 +69,7 @@ __device__ __forceinline__ void scores(const char* t0, const char* t1, int row0,
     }
     keep_order();
     if (g >= 0) {
+      tick(g);
 #pragma unroll
       for (int n = 0; n < GK; ++n) {
         const int c = g * GK + n;
@@ -149,7 +150,9 @@ constexpr int kExactKeys = 512;
 // WIDE and its other form: as in the forward.
 template <int DT, int KC, int VT, bool WIDE>
 __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_bwd_queries(BwdArgs f) {
-  constexpr int BN = step_of<DT, WIDE>(), kBM = WIDE ? kWideRows : 32, NB = WIDE ? BN / 32 : 1, KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
+  constexpr int BN = step_of<DT, WIDE>(), kBM = WIDE ? kWideRows : 32, NB = WIDE ? BN / 32 : 1;
+  constexpr bool SPREAD = WIDE && DT != kDtF32;  // as in the forward
+  constexpr int KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
   constexpr int SG = DT == kDtF32 ? 1 : KC > 8 ? 2 : 4;  // fragments read ahead: two waves a SIMD leave 256 registers
   constexpr int KB = tile_bytes<DT, BN, KW>(), TB = KB + tile_bytes<DT, BN, VW>(), ES = esize<DT>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -183,6 +186,18 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
     tile_load<DT, BN, KW, kThreads>(t, kp + j0 * a.k_t * ES, a.k_t, a.d_nope, rp + j0 * a.kr_t * ES, a.kr_t, a.d_rope,
                                     nk - j0, f.vec, tid);
     tile_load<DT, BN, VW, kThreads>(t + KB, vp + j0 * a.v_t * ES, a.v_t, dv, nullptr, 0, 0, nk - j0, f.vec, tid);
+  };
+  constexpr int R4 = 256 / pieces<DT>();  // (BN where SPREAD)
+  TileLoads<DT, R4, KW, kThreads> kl;
+  TileLoads<DT, R4, VW, kThreads> vl;
+  constexpr int LOADS = SPREAD ? kl.LOADS + vl.LOADS : 0;
+  auto tick = [&](int n) {
+    if constexpr (SPREAD) {
+      if (n < kl.LOADS)
+        kl.load(n);
+      else if (n < LOADS)
+        vl.load(n - kl.LOADS);
+    }
   };
   if (n_end > 0) issue(0, smem);
   const int64_t row = static_cast<int64_t>(q_lo + min(i, nq - 1)) * a.H + h;
@@ -227,10 +242,17 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
         at ^= 1;
         wait_loads();
         lds_barrier();
-        if (j0 + BN < n_end)
-          issue(j0 + BN, smem + at * TB);
-        else if (more)
-          issue(0, smem + at * TB);
+        char* to = smem + at * TB;
+        if constexpr (SPREAD) {
+          // (after the last tile, the first: no branch between the products)
+          const int jn = j0 + BN < n_end ? j0 + BN : 0;
+          kl.start(to, kp + jn * a.k_t * ES, a.k_t, a.d_nope, rp + jn * a.kr_t * ES, a.kr_t, a.d_rope, nk - jn, tid);
+          vl.start(to + KB, vp + jn * a.v_t * ES, a.v_t, dv, nullptr, 0, 0, nk - jn, tid);
+        } else if (j0 + BN < n_end) {
+          issue(j0 + BN, to);
+        } else if (more) {
+          issue(0, to);
+        }
       } else {
         if (at > 0) {
           lds_barrier();
@@ -240,16 +262,24 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
         wait_loads();
         lds_barrier();
       }
-      if (j0 + rb >= w_end) continue;
+      if (j0 + rb >= w_end) {
 #pragma unroll
-      for (int b = 0; b < NB; ++b) block(kt, kt + KB, rb + 32 * b, j0 + rb + 32 * b);
+        for (int n = 0; n < LOADS; ++n) tick(n);
+        continue;
+      }
+      // (the loads between the score products of the blocks: NG groups each)
+      constexpr int NG = (KC + 2 * VT + SG - 1) / SG;
+      static_assert(!SPREAD || NB * NG >= LOADS, "a place for every load");
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        block(kt, kt + KB, rb + 32 * b, j0 + rb + 32 * b, [&](int g) { tick(b * NG + g); });
     }
   };
   if (n_end <= kExactKeys) {
     float d = 0.0f;
-    walk(true, [&](const char* kt, const char* vt, int r0, int j) {
+    walk(true, [&](const char* kt, const char* vt, int r0, int j, auto&& between) {
       floatx16 s, dp;
-      scores<DT, KC, 2 * VT, BN, SG>(kt, vt, r0, lane, qf, df, s, dp);
+      scores<DT, KC, 2 * VT, BN, SG>(kt, vt, r0, lane, qf, df, s, dp, between);
       probabilities(j, s);
 #pragma unroll
       for (int e = 0; e < 16; ++e) d += s[e] == 0.0f ? 0.0f : s[e] * dp[e];
@@ -269,14 +299,15 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) gq[t][e] = 0.0f;
-  walk(false, [&](const char* kt, const char* vt, int r0, int j) {
+  walk(false, [&](const char* kt, const char* vt, int r0, int j, auto&& between) {
     floatx16 s, dp;
-    scores<DT, KC, 2 * VT, BN, SG>(kt, vt, r0, lane, qf, df, s, dp);
+    scores<DT, KC, 2 * VT, BN, SG>(kt, vt, r0, lane, qf, df, s, dp, between);
     probabilities(j, s);
 #pragma unroll
     for (int e = 0; e < 16; ++e) dp[e] = s[e] == 0.0f ? 0.0f : s[e] * (dp[e] - del) * fac;
     add_products<DT, KT, BN, SG>(kt, r0, lane, dp, gq);
   });
+  if constexpr (SPREAD) wait_loads();  // none may arrive after the workgroup's end
   const float qs = a.scale / fac;
   char* gp = static_cast<char*>(a.dq) + row * dk * ES;
 #pragma unroll
@@ -296,7 +327,8 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   }
 }
 
-// keys: dK, dV
+// keys: dK, dV.  (The loads of a step all at once: one at a time between the products, as for
+// the queries, they take registers that the accumulators and operands do not leave.)
 // Not WIDE: the four waves share 32 keys and split the queries.
 template <int DT, int KC, int VT, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
@@ -409,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       floatx16 s, dp;
-      scores<DT, KC, 2 * VT, BQ>(qt, dt, rb + 32 * b, lane, kf, vf, s, dp);
+      scores<DT, KC, 2 * VT, BQ, DT == kDtF32 ? 1 : 4>(qt, dt, rb + 32 * b, lane, kf, vf, s, dp, [](int) {});
       const bool mask = a.causal && i_here + 32 * b + off < j0 + w0 + 31;
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
@@ -509,9 +541,10 @@ hipError_t bwd_form(const BwdArgs& f, int T, const int32_t* cu, int heads, hipSt
   // other (7B heads, bf16): 160 workgroups (512 rows) 85 against 70, 91 against 85; 192 (4 x 512) 51 against
   // 51, 49 against 51; 224 (768) 109 against 107, 103 against 109; 288 (1024) 141 against 154, 118 against
   // 141; fp32, 64 wide, 136 (2048): 360 against 223, 543 against 360.  Four queries' heads a key head: 136
-  // 422 against 257 for the keys.  (The widest fp32 heads' 128 rows do not fit.)
+  // 422 against 257 for the keys.  (The widest fp32 heads' 128 rows do not fit.  16-bit rows that fit
+  // no 16-byte loads take the other form.)
   if constexpr (lds_of<DT, KC, VT, false>(!QUERIES) <= kLdsMax) {
-    if (wide_groups(T, cu ? f.a.n_seq : 0, heads) < (DT == kDtF32 ? 400 : 210))
+    if (wide_groups(T, cu ? f.a.n_seq : 0, heads) < (DT == kDtF32 ? 400 : 210) || (DT != kDtF32 && !f.vec))
       return bwd_one<DT, KC, VT, QUERIES, false>(f, T, cu, heads, stream);
   }
   return bwd_one<DT, KC, VT, QUERIES, true>(f, T, cu, heads, stream);
