@@ -8,6 +8,15 @@
 // holds their K and V as B operands in registers and walks the queries of all heads
 // that share it; the other owns 128 queries and walks their keys.  The shared rotary
 // key's gradient is summed over the key heads from fp32 partial results.
+//
+// Bound by the matrix cores (4 dk + 4 dv operations a pair of query and key in the keys' kernel,
+// 4 dk + 2 dv in the queries') and by what a wave does between them.  Measured (two sequences of
+// 2048 tokens, 7B heads, 128 + 64 wide keys, bf16): queries 203 to 222 us, keys 341 to 355 us; with
+// the forward (126 to 135 us) about 450 TFLOP/s of the least work.  The matrix cores are busy
+// 35 and 27% of the cycles: a wave's operands and sums leave room for one wave on a SIMD, so
+// that nothing runs beside its loads and exponentials (of 7600 cycles of a step of the keys' kernel
+// 2200 issue loads, 2700 are scores and exponentials, 1900 the last products).  Two waves a
+// SIMD that share the keys and pass P and dS through LDS were no faster (358 us).
 #include "attn.h"
 #include "attn_common.h"
 
@@ -182,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   const char* kp = static_cast<const char*>(a.k) + (k_lo * a.k_t + kvh * a.k_h) * ES;
   const char* vp = static_cast<const char*>(a.v) + (k_lo * a.v_t + kvh * a.v_h) * ES;
   const char* rp = static_cast<const char*>(a.k_rope) + k_lo * a.kr_t * ES;
-  auto issue = [&](int j0, char* t) {
+  auto issue = [&](int j0, char* t) __attribute__((always_inline)) {
     tile_load<DT, BN, KW, kThreads>(t, kp + j0 * a.k_t * ES, a.k_t, a.d_nope, rp + j0 * a.kr_t * ES, a.kr_t, a.d_rope,
                                     nk - j0, f.vec, tid);
     tile_load<DT, BN, VW, kThreads>(t + KB, vp + j0 * a.v_t * ES, a.v_t, dv, nullptr, 0, 0, nk - j0, f.vec, tid);
@@ -191,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   TileLoads<DT, R4, KW, kThreads> kl;
   TileLoads<DT, R4, VW, kThreads> vl;
   constexpr int LOADS = SPREAD ? kl.LOADS + vl.LOADS : 0;
-  auto tick = [&](int n) {
+  auto tick = [&](int n) __attribute__((always_inline)) {
     if constexpr (SPREAD) {
       if (n < kl.LOADS)
         kl.load(n);
@@ -225,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
     del += __shfl_xor(del, 32);
   }
   // P in s, from S; the mask where the block reaches past a query's last key
-  auto probabilities = [&](int j, floatx16& s) {
+  auto probabilities = [&](int j, floatx16& s) __attribute__((always_inline)) {
     const bool mask = j + 31 > lim_lo;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -235,7 +244,8 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   };
   int at = 0;  // the tile that is read (the other form: whether it has been read)
   // the keys' tiles in turn; the last step issues the first tile again if `more`
-  auto walk = [&](bool more, auto&& block) {
+  // (inlined by force: in the fp32 kernels the compiler made calls of these, through scratch)
+  auto walk = [&](bool more, auto&& block) __attribute__((always_inline)) {
     for (int j0 = 0; j0 < n_end; j0 += BN) {
       char* kt = smem + (WIDE ? at * TB : 0);
       if constexpr (WIDE) {
@@ -277,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   };
   if (n_end <= kExactKeys) {
     float d = 0.0f;
-    walk(true, [&](const char* kt, const char* vt, int r0, int j, auto&& between) {
+    walk(true, [&](const char* kt, const char* vt, int r0, int j, auto&& between) __attribute__((always_inline)) {
       floatx16 s, dp;
       scores<DT, KC, 2 * VT, BN, SG>(kt, vt, r0, lane, qf, df, s, dp, between);
       probabilities(j, s);
@@ -299,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) gq[t][e] = 0.0f;
-  walk(false, [&](const char* kt, const char* vt, int r0, int j, auto&& between) {
+  walk(false, [&](const char* kt, const char* vt, int r0, int j, auto&& between) __attribute__((always_inline)) {
     floatx16 s, dp;
     scores<DT, KC, 2 * VT, BN, SG>(kt, vt, r0, lane, qf, df, s, dp, between);
     probabilities(j, s);
