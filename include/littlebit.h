@@ -579,7 +579,7 @@ lb_status lb_attention_forward(const lb_attention* a, void* o, float* lse, hipSt
    not accumulated, rounded once from fp32 sums.  o and lse are the forward's.
    P and dS are rounded to dtype for their products.  Gradients of grouped heads
    are summed in a fixed order: repeated calls give the same bits.  No output may
-   overlap an input or another output (not checked).  workspace: 256-byte
+   overlap an input or another output (not checked).  If H is 0 nothing is written.  workspace: 256-byte
    aligned, >= lb_attention_backward_workspace_bytes(Tq, Tk, H, Hk, d_rope)
    bytes (0 for invalid sizes), no zero-fill needed. */
 typedef struct lb_attention_grads {

@@ -3,6 +3,10 @@
 //   P = exp(S - lse), D = rowsum(dO (.) O), dS = P (.) (dO V^T - D)
 //   dV = P^T dO, dK = scale dS^T Q_n, dK_rope = scale sum over heads dS^T Q_r, dQ = scale dS [K | K_rope]
 //
+// P and dS enter their products as one value of the call's type: each has the relative rounding
+// of the results themselves, so a gradient is off by about sqrt(2) of its own rounding (measured
+// 1.40 to 1.5).  A second term of dS would double dQ's products for the rest.
+//
 // Two kernels (queries, then keys), each forming S and dO V^T anew, so that every gradient is summed by
 // one owner in a fixed order (no atomics on values): one owns 128 keys of a key head,
 // holds their K and V as B operands in registers and walks the queries of all heads
@@ -11,11 +15,11 @@
 //
 // Bound by the matrix cores (4 dk + 4 dv operations a pair of query and key in the keys' kernel,
 // 4 dk + 2 dv in the queries') and by what a wave does between them.  Measured (two sequences of
-// 2048 tokens, 7B heads, 128 + 64 wide keys, bf16): queries 203 to 222 us, keys 341 to 355 us; with
-// the forward (126 to 135 us) about 450 TFLOP/s of the least work.  The matrix cores are busy
-// 35 and 27% of the cycles: a wave's operands and sums leave room for one wave on a SIMD, so
-// that nothing runs beside its loads and exponentials (of 7600 cycles of a step of the keys' kernel
-// 2200 issue loads, 2700 are scores and exponentials, 1900 the last products).  Two waves a
+// 2048 tokens, 7B heads, 128 + 64 wide keys, bf16): queries 203 to 228 us, keys 341 to 370 us; with
+// the forward (126 to 142 us) about 450 TFLOP/s of the least work.  The matrix cores are busy
+// 48 and 30% of the CUs' cycles: the keys' wave holds so many operands and sums that one fits
+// a SIMD, and nothing runs beside its loads and exponentials (of 7600 cycles of a step 2200
+// issue loads, 2700 are scores and exponentials, 1900 the last products).  Two waves a
 // SIMD that share the keys and pass P and dS through LDS were no faster (358 us).
 #include "attn.h"
 #include "attn_common.h"
