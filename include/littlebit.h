@@ -577,7 +577,8 @@ lb_status lb_attention_forward(const lb_attention* a, void* o, float* lse, hipSt
    like q; dk, dv with the given strides (rows must not overlap); dk_rope [Tk x
    d_rope], summed over all heads (NULL if d_rope is 0); all of dtype, written,
    not accumulated, rounded once from fp32 sums.  o and lse are the forward's.
-   P and dS are rounded to dtype for their products.  Gradients of grouped heads
+   P and dS are rounded to dtype for their products (dS for dq of heads up to 128
+   wide to two terms of it).  Gradients of grouped heads
    are summed in a fixed order: repeated calls give the same bits.  No output may
    overlap an input or another output (not checked).  If H is 0 nothing is written.  workspace: 256-byte
    aligned, >= lb_attention_backward_workspace_bytes(Tq, Tk, H, Hk, d_rope)

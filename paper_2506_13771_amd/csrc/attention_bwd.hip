@@ -3,9 +3,11 @@
 //   P = exp(S - lse), D = rowsum(dO (.) O), dS = P (.) (dO V^T - D)
 //   dV = P^T dO, dK = scale dS^T Q_n, dK_rope = scale sum over heads dS^T Q_r, dQ = scale dS [K | K_rope]
 //
-// P and dS enter their products as one value of the call's type: each has the relative rounding
-// of the results themselves, so a gradient is off by about sqrt(2) of its own rounding (measured
-// 1.40 to 1.5).  A second term of dS would double dQ's products for the rest.
+// P and dS enter the keys' products as one value of the call's type: each has the relative
+// rounding of the results themselves, so a gradient is off by about sqrt(2) of its own rounding
+// (measured 1.41 to 1.45).  dQ adds what D has from the rounded O (up to 1.5), so its dS enters in two
+// terms (1.00 to 1.03 then) for heads up to 128 wide; wider ones (1.45 at 192) have no registers
+// left and would pay 17% of their kernel (217 -> 254 us of 2 x 2048 tokens of 7B heads).
 //
 // Two kernels (queries, then keys), each forming S and dO V^T anew, so that every gradient is summed by
 // one owner in a fixed order (no atomics on values): one owns 128 keys of a key head,
@@ -95,17 +97,22 @@ __device__ __forceinline__ void scores(const char* t0, const char* t1, int row0,
   }
 }
 // acc[t] += (columns 32 t .. of the tile's rows row0 .. row0 + 31)^T x, x the block's
-// accumulator as B operand
-template <int DT, int T, int R, int MOST = 4>
+// accumulator as B operand, in TERMS terms of the type
+template <int DT, int T, int R, int MOST = 4, int TERMS = 1>
 __device__ __forceinline__ void add_products(const char* tile, int row0, int lane, const floatx16& x, floatx16 (&acc)[T]) {
   constexpr int GK = DT == kDtF32 ? 1 : T % 4 == 0 && MOST >= 4 ? 4 : T % 3 == 0 && MOST >= 3 ? 3 : 2, NG = 2 * T / GK;
-  Frag<DT> f[2][GK], xf[2];
+  Frag<DT> f[2][GK], xf[TERMS][2];
 #pragma unroll
   for (int sl = 0; sl < 2; ++sl) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = x[8 * sl + e];
-    xf[sl] = frag_from<DT>(v);
+    xf[0][sl] = frag_from<DT>(v);
+    if constexpr (TERMS > 1) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] -= frag_elem<DT>(xf[0][sl], e);
+      xf[1][sl] = frag_from<DT>(v);
+    }
   }
 #pragma unroll
   for (int g = -1; g < NG; ++g) {
@@ -121,7 +128,14 @@ __device__ __forceinline__ void add_products(const char* tile, int row0, int lan
 #pragma unroll
       for (int n = 0; n < GK; ++n) {
         const int c = g * GK + n;
-        acc[c % T] = mma32<DT>(f[g & 1][n], xf[c / T], acc[c % T]);
+        acc[c % T] = mma32<DT>(f[g & 1][n], xf[0][c / T], acc[c % T]);
+      }
+      if constexpr (TERMS > 1) {
+#pragma unroll
+        for (int n = 0; n < GK; ++n) {
+          const int c = g * GK + n;
+          acc[c % T] = mma32<DT>(f[g & 1][n], xf[1][c / T], acc[c % T]);
+        }
       }
     }
   }
@@ -166,6 +180,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   constexpr int BN = step_of<DT, WIDE>(), kBM = WIDE ? kWideRows : 32, NB = WIDE ? BN / 32 : 1;
   constexpr bool SPREAD = WIDE && DT != kDtF32;  // as in the forward
   constexpr int KW = 16 * KC, VW = 32 * VT, KT = KC / 2;
+  constexpr int DST = DT == kDtF32 || KC > 8 ? 1 : 2;  // terms of dS
   constexpr int SG = DT == kDtF32 ? 1 : KC > 8 ? 2 : 4;  // fragments read ahead: two waves a SIMD leave 256 registers
   constexpr int KB = tile_bytes<DT, BN, KW>(), TB = KB + tile_bytes<DT, BN, VW>(), ES = esize<DT>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -319,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
     probabilities(j, s);
 #pragma unroll
     for (int e = 0; e < 16; ++e) dp[e] = s[e] == 0.0f ? 0.0f : s[e] * (dp[e] - del) * fac;
-    add_products<DT, KT, BN, SG>(kt, r0, lane, dp, gq);
+    add_products<DT, KT, BN, SG, DST>(kt, r0, lane, dp, gq);
   });
   if constexpr (SPREAD) wait_loads();  // none may arrive after the workgroup's end
   const float qs = a.scale / fac;
