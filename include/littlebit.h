@@ -471,7 +471,8 @@ lb_status lb_dual_svid(const void* W, lb_dtype w_dtype, int64_t d_out, int64_t d
        cu[b] .. cu[b + 1] - 1 of w and q belong to sequence b, as its last
        positions lens[b] - (cu[b + 1] - cu[b]) .. lens[b] - 1.
    The kernels keep every access inside the buffers whatever these arrays hold:
-   lens are cut to max_pages page_size; a token without a place (before
+   sequence b's rows begin where those of the sequences before it end, also where cu falls (no row is
+   in two sequences); lens are cut to max_pages page_size; a token without a place (before
    position 0, past the table, or on a page outside [0, n_pages)) is not written
    and not seen; rows behind cu[n_seq] are neither read nor written.  A place
    named twice in one append holds parts of either token.

@@ -26,14 +26,13 @@
 // chain of dependent loads; 1440 columns, 8 sequences of 1000 to 4000: 9.4 + 36 + 17.6.
 #include "attn.h"
 #include "attn_common.h"
+#include "latent_map.h"
 
 namespace lb {
 
 namespace {
 
 constexpr size_t kLdsMax = 163840;
-constexpr int kCols = 32;  // query rows of an item (columns of the tiles)
-constexpr int kG = 256;    // workgroups of split (one a CU)
 
 // ---------------------------------------------------------------------------
 // plan (host)
@@ -99,7 +98,7 @@ struct LatWs {
 __host__ LatWs lat_ws(int64_t T, int64_t n_seq, int64_t H, int r, int d_rope) {
   LatWs w{};
   const int64_t row = latent_row(r, d_rope), ow = (2 * r + 31) / 32 * 32;
-  const int64_t slots = kG + (T * H + kCols - 1) / kCols + n_seq;
+  const int64_t slots = lat_slots(T, n_seq, H);
   auto up = [](size_t b) { return (b + 255) / 256 * 256; };
   w.qs_off = up(static_cast<size_t>((T * H + kCols - 1) / kCols * kCols * row) * 6);
   w.ml_off = w.qs_off + up(static_cast<size_t>(T * H) * 4);
@@ -110,21 +109,17 @@ __host__ LatWs lat_ws(int64_t T, int64_t n_seq, int64_t H, int r, int d_rope) {
 
 // ---------------------------------------------------------------------------
 // work map: sequence b has ceil(nq_b H / 32) items of ceil(len_b / step) steps each;
-// all W steps in a row are dealt to G workgroups (G <= W), g taking [W g / G, W (g + 1) / G);
-// its part of the item numbered i over all sequences goes to slot g + i, so that an
-// item's slots are consecutive and no two meet.  Sums stay below 2^31 (the caller's
-// sizes are checked for it).
+// all W steps in a row are dealt to G workgroups (latent_map.h).
 // ---------------------------------------------------------------------------
 struct SeqWork {
   int q0, nq;       // first token, tokens
   int len;          // cached tokens, within the page table
   int items, steps;  // items, steps of each
 };
-__device__ __forceinline__ SeqWork seq_work(const CacheArgs& c, int b, int T, int H, int step) {
+// sequence b, whose tokens are rows q0 .. q0 + nq - 1
+__device__ __forceinline__ SeqWork seq_work(const CacheArgs& c, int b, int q0, int nq, int H, int step) {
   SeqWork s;
-  int hi;
-  seq_range(c.cu, b, T, s.q0, hi);
-  s.nq = hi - s.q0;
+  s.q0 = q0, s.nq = nq;
   s.len = max(0, min(c.lens[b], c.max_pages * c.page_size));
   s.items = (s.nq * H + kCols - 1) / kCols;
   // step is 16, 32, 64 or 128
@@ -149,11 +144,23 @@ struct WorkMap {
   int block = -1;  // the 64 sequences held
   SeqWork s;
   int ws, is;      // inclusive sums of steps and items over them
-  __device__ __forceinline__ void hold(int b0) {
+  int end;         // the row behind the last of them
+  // before: the row behind the sequences before b0 (of the first 64: what cu says)
+  __device__ __forceinline__ void hold(int b0, int before) {
     if (b0 == block) return;
     block = b0;
+    const int b = b0 + lane;
+    if (b0 == 0) before = rows_end(0, c.cu[0], T);
+    int hi = rows_end(before, b < c.n_seq ? c.cu[b + 1] : 0, T), lo = before;
+    if (c.n_seq > 1) {
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) hi = max(hi, __shfl_up(hi, d));  // (a lane below d gets its own)
+      lo = __shfl_up(hi, 1);
+      if (lane == 0) lo = before;
+    }
+    end = __builtin_amdgcn_readlane(hi, 63);
     s = SeqWork{0, 0, 0, 0, 0};
-    if (b0 + lane < c.n_seq) s = seq_work(c, b0 + lane, T, H, step);
+    if (b < c.n_seq) s = seq_work(c, b, lo, hi - lo, H, step);
     ws = s.items * s.steps, is = s.items;
     if (c.n_seq > 1) {
 #pragma unroll
@@ -165,9 +172,10 @@ struct WorkMap {
   }
   __device__ __forceinline__ int last() const { return min(63, c.n_seq - 1 - block); }
   __device__ __forceinline__ int total() {
-    int w = 0;
-    for (int b0 = (c.n_seq - 1) / 64 * 64; b0 >= 0; b0 -= 64) {  // block 0 last: it stays held
-      hold(b0);
+    int w = 0, before = 0;
+    for (int b0 = 0; b0 < c.n_seq; b0 += 64) {
+      hold(b0, before);
+      before = end;
       w += __builtin_amdgcn_readlane(ws, last());
     }
     return w;
@@ -176,8 +184,10 @@ struct WorkMap {
   // its index (-1: none), its work, and the steps and items before it.
   __device__ __forceinline__ int find(bool by_step, int x, SeqWork& out, int& sb, int& ib) {
     sb = 0, ib = 0;
+    int before = 0;
     for (int b0 = 0; b0 < c.n_seq; b0 += 64) {
-      hold(b0);
+      hold(b0, before);
+      before = end;
       const uint64_t m = __ballot(b0 + lane < c.n_seq && (by_step ? sb + ws > x : s.q0 <= x && x < s.q0 + s.nq));
       if (m != 0) {
         const int k = __builtin_ctzll(m);
@@ -192,22 +202,6 @@ struct WorkMap {
     return -1;
   }
 };
-// Workgroups that W steps are dealt to: at least 128 tokens each, since a share's
-// partial result (32 rows of 4-byte sums, written and read again) costs as much memory
-// traffic as 128 tokens of a 16-bit cache.
-__device__ __forceinline__ int groups_of(int W, int step) {
-  return max(1, min(kG, W / max(1, 128 / step)));
-}
-// (quotients of integers below 2^40 in 64 bits: a floor is exact, the nearest wrong
-// integer being 2^-31 or more away)
-__device__ __forceinline__ int first_step(int W, int g, int G) {
-  return static_cast<int>(static_cast<double>(static_cast<int64_t>(W) * g) / static_cast<double>(G));
-}
-// the workgroup that step x belongs to
-__device__ __forceinline__ int group_of(int W, int x, int G) {
-  return static_cast<int>(static_cast<double>((static_cast<int64_t>(x) + 1) * G - 1) / static_cast<double>(W));
-}
-
 // n / d for 0 <= n < 2^31 by a multiplication: m = ceil(2^(31 + l) / d), l = ceil(log2 d) (m = 0: d = 1)
 struct Divisor {
   uint32_t m, shift;
