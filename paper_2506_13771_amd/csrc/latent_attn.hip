@@ -497,6 +497,9 @@ __device__ __forceinline__ Frag<CD> tile_cols(const char* t, int s, int lane) {
   return f;
 }
 
+// a cache row of zeros (the widest, 4 bytes a column)
+__device__ const uint32_t kZeroRow[kMaxLatentRow] = {};
+
 template <int CD, int TQ, int TP, int UPW, bool CSPLIT>
 __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -522,6 +525,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
   float* xchg = reinterpret_cast<float*>(smem + (CSPLIT ? 4 : p.ntw) * p.stages * p.tile_bytes);
   const int64_t row_bytes = static_cast<int64_t>(c.row) * esize<CD>();
   const char* data = static_cast<const char*>(c.data) + u0 * 32 * esize<CD>();
+  const char* zeros = reinterpret_cast<const char*>(kZeroRow) + u0 * 32 * esize<CD>();
   const int ow = p.vu * 32, unit_bytes = p.tpt * PU * 16;
 
   while (x < x_end) {
@@ -535,9 +539,9 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
     const int s1 = min(sw.steps, s0 + (x_end - x));
     const int64_t slot = g + ib + item;
 
-    // a token's page; its row of the cache, where the page is one.  Token 0 stands in for
-    // tokens without a place: every row sees it, so that what the masked scores' zero
-    // probabilities are multiplied with is no stranger's infinity.
+    // a token's page; its row of the cache, where the page is one.  Tokens without a place
+    // (and those past the end) read zeros, so that what the masked scores' zero probabilities
+    // are multiplied with is no stranger's infinity.
     const int32_t* table = c.table + static_cast<int64_t>(b) * c.max_pages;
     auto page_of = [&](int tok) { return table[quotient(min(tok, sw.len - 1), a.page)]; };
     auto place = [&](int tok, int page, bool& ok) {
@@ -546,24 +550,21 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
     };
     auto tile_at = [&](int s) { return (s * p.ntw + tw) * p.tpt; };
     int page = page_of(tile_at(s0) + ml_);
-    const int page0 = table[0];
 
-    bool ok0;
-    const int at0 = place(0, page0, ok0);
-    const int place0 = ok0 ? at0 : 0;
     // A tile's loads, 64 / PU tokens each: lane l takes piece l % PU of rows l / PU + n 64 / PU.
     // Returns which of the tile's tokens are seen.
     constexpr int TPL = 64 / PU, NL = 32 / TPL;  // tokens of a load, loads of a unit of 32 tokens
     auto issue = [&](int tok, int pg, char* dst) -> uint32_t {
       bool ok;
       const int at = place(tok, pg, ok);
-      const int idx = ok ? at : place0;
+      const int idx = ok ? at : -1;
       ok = ok && ml_ < p.tpt;
       const char* src[NL];
 #pragma unroll
       for (int n = 0; n < NL; ++n) {
         const int t = lane / PU + n * TPL;
-        src[n] = data + __shfl(idx, t & (p.tpt - 1)) * row_bytes + 16 * ((lane & (PU - 1)) ^ unit_swz<CD>(t));
+        const int of = __shfl(idx, t & (p.tpt - 1));
+        src[n] = (of < 0 ? zeros : data + of * row_bytes) + 16 * ((lane & (PU - 1)) ^ unit_swz<CD>(t));
       }
 #pragma unroll
       for (int u = 0; u < UPW; ++u) {
@@ -883,13 +884,13 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
   float l = 0.0f;
   for (int i = lane; i < n; i += 64) {
     const float* q = j.ml + ((slot0 + i) * kCols + m) * 2;
-    const float f = top == -INFINITY ? 0.0f : exp2_fast(q[0] - top);
-    l += f * q[1];
+    const float f = top == -INFINITY ? 1.0f : exp2_fast(q[0] - top);
+    l += f * q[1];  // (0: no token is seen)
     if (tid < 64) wt[i] = f;
   }
 #pragma unroll
   for (int s = 32; s > 0; s >>= 1) l += __shfl_xor(l, s);
-  const float inv = top == -INFINITY ? 0.0f : 1.0f / l;
+  const float inv = 1.0f / l;
   for (int i = tid; i < 2 * (rp - r); i += kJThreads) {
     const int p = i >= rp - r;
     ov[p][r + i - p * (rp - r)] = 0.0f;
@@ -900,7 +901,7 @@ __global__ void __launch_bounds__(kJThreads) join_kernel(JoinArgs j) {
     float v = 0.0f;
 #pragma unroll 8
     for (int i = 0; i < n; ++i) v += wt[i] * po[static_cast<int64_t>(i) * kCols * ow + k];
-    ov[k >= r][k >= r ? k - r : k] = v * inv;
+    ov[k >= r][k >= r ? k - r : k] = l == 0.0f ? 0.0f : v * inv;
   }
   __syncthreads();
   if (ph < 2 * KPARTS) {

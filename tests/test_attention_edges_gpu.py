@@ -59,3 +59,80 @@ def test_latent_attention_with_sums_that_fall(lens, T, cu, rows, act):
             ref, bound = R.latent_attention(q[lo:hi], [P.rows[b]], up, H, dv, [lens[b]], [hi - lo], f, dr,
                                             (dn + dr) ** -0.5, DT[act])
             _within(out[lo:hi], ref, bound, (b, lo, hi))
+
+
+# ----------------------------------------------------------------------------
+# tokens without a place
+# ----------------------------------------------------------------------------
+def _free_page_0(P):
+    """Page 0 of the pool belongs to no sequence and holds NaN."""
+    used = (P.table == 0).nonzero()
+    if len(used):
+        taken = set(P.table.flatten().tolist())
+        other = next(i for i in range(P.data.shape[0]) if i not in taken)
+        P.data[other] = P.data[0]
+        P.table[tuple(used[0])] = other
+    P.data[0] = float("nan")
+    P.cache.data.copy_(P.data)
+
+
+MISSING = [  # lens, H, dn, dv, r, dr, page, act, cache
+    ([40, 100, 9], 4, 32, 32, 24, 0, 8, "f32", "f32"),
+    ([40, 100, 300], 32, 64, 64, 112, 64, 16, "bf16", "bf16"),
+    ([70, 33, 20], 5, 32, 32, 64, 32, 7, "f16", "f16"),
+    ([70, 130, 20], 3, 32, 32, 400, 64, 16, "bf16", "bf16"),   # four column waves
+    ([70, 130, 20], 2, 32, 32, 700, 32, 16, "f32", "f32"),
+]
+
+
+@pytest.mark.parametrize("case", MISSING, ids=lambda c: f"r{c[4]}-{c[7]}-{c[8]}")
+def test_first_pages_that_are_missing(case):
+    # sequence 0 has lost its first page and a later one, sequence 1 its first three (a window that has moved on),
+    # sequence 2 all of them
+    lens, H, dn, dv, r, dr, page, act, cd = case
+    g = _gen(r)
+    P = Paged(g, lens, [1, 1, 1], r, dr, page, cd)
+    _free_page_0(P)
+    gone = {0: [0, 2], 1: [0, 1, 2], 2: list(range(P.table.shape[1]))}
+    rows = []
+    for b, pages in gone.items():
+        keep = torch.ones(lens[b], dtype=torch.bool)
+        for i in pages:
+            P.table[b, i] = (-1, 0x7fffffff, P.data.shape[0], -(2 ** 31))[i % 4]
+            keep[i * page:(i + 1) * page] = False
+        keep[lens[b] - 1] &= True
+        rows.append(P.rows[b][keep])
+    paths, up = _layer(g, r, H * (dn + dv))
+    q, f = _normal(g, 3, H, dn + dr, dtype=act), _freqs(dr) if dr else None
+    out = lb.lb_latent_attention(q.cuda(), P.cache, paths, H, dv, P.table.cuda(), P.meta[1], P.meta[2],
+                                 None if f is None else f.cuda())
+    assert bool((out[2] == 0).all())
+    for b in range(2):
+        # (the query turned by its position among all tokens: the reference gets it turned)
+        qb = q[b:b + 1].double()
+        if dr:
+            qb = torch.cat([qb[..., :dn], R.turn(qb[..., dn:], _ints([lens[b] - 1]), f)], -1)
+        n = rows[b].shape[0]
+        ref, bound = _turned_reference(qb, q[b:b + 1], rows[b], up, H, dv, n, dr, (dn + dr) ** -0.5, DT[cd])
+        _within(out[b:b + 1], ref, bound, (b, n))
+
+
+def _turned_reference(turned, q, rows, up, H, dv, n, dr, scale, cd):
+    """attn_ref's reference of one query over n rows, its rotary part given turned (fp64)."""
+    class Q:  # a tensor of q's type that reads as the turned values
+        dtype, shape = q.dtype, q.shape
+
+        def __getitem__(self, i):
+            return turned[i]
+    return R.latent_attention(Q(), [rows], up, H, dv, [n], [1], None, dr, scale, cd)
+
+
+def test_queries_before_the_first_token_stay_0():
+    # four new tokens of a sequence of two: the first two queries see nothing, whatever the cache's rows hold
+    lens, H, dn, dv, r = [2], 4, 32, 32, 24
+    g = _gen(77)
+    P = Paged(g, lens, [4], r, 0, 8, "f32")
+    P.cache.data[int(P.table[0, 0])] = float("inf")
+    paths, _ = _layer(g, r, H * (dn + dv))
+    out = lb.lb_latent_attention(_normal(g, 4, H, dn).cuda(), P.cache, paths, H, dv, *P.meta)
+    assert bool((out[:2] == 0).all()) and bool(torch.isnan(out[2:]).all())
