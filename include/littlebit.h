@@ -469,12 +469,13 @@ lb_status lb_dual_svid(const void* W, lb_dtype w_dtype, int64_t d_out, int64_t d
      lens [n_seq]: cached tokens of each sequence, the call's new ones included;
      cu [n_seq + 1]: prefix sums of the call's new tokens, cu[0] = 0: token rows
        cu[b] .. cu[b + 1] - 1 of w and q belong to sequence b, as its last
-       positions lens[b] - (cu[b + 1] - cu[b]) .. lens[b] - 1.
+       positions lens[b] - (cu[b + 1] - cu[b]) .. lens[b] - 1, whether or not
+       the table has room for them.
    The kernels keep every access inside the buffers whatever these arrays hold:
    sequence b's rows begin where those of the sequences before it end, also where cu falls (no row is
-   in two sequences); lens are cut to max_pages page_size; a token without a place (before
-   position 0, past the table, or on a page outside [0, n_pages)) is not written
-   and not seen; rows behind cu[n_seq] are neither read nor written.  A place
+   in two sequences); a token without a place (before
+   position 0, past the table's max_pages page_size, or on a page outside [0, n_pages)) is not written
+   and not seen, and the places of the others do not depend on it; rows behind cu[n_seq] are neither read nor written.  A place
    named twice in one append holds parts of either token.
    2 r + d_rope <= 1536, d_rope even and <= 256, n_pages page_size < 2^31 and
    max_pages page_size <= 2^30 (LB_ERR_SHAPE); data may be larger than 2^31

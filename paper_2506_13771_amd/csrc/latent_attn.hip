@@ -113,6 +113,7 @@ __host__ LatWs lat_ws(int64_t T, int64_t n_seq, int64_t H, int r, int d_rope) {
 // ---------------------------------------------------------------------------
 struct SeqWork {
   int q0, nq;       // first token, tokens
+  int first;        // the first one's position (below 0: it has none)
   int len;          // cached tokens, within the page table
   int items, steps;  // items, steps of each
 };
@@ -120,7 +121,10 @@ struct SeqWork {
 __device__ __forceinline__ SeqWork seq_work(const CacheArgs& c, int b, int q0, int nq, int H, int step) {
   SeqWork s;
   s.q0 = q0, s.nq = nq;
-  s.len = max(0, min(c.lens[b], c.max_pages * c.page_size));
+  const int n = max(0, c.lens[b]);
+  // as lb_latent_append places them: row t at lens[b] - (cu[b + 1] - t)
+  s.first = nq > 0 ? n - (c.cu[b + 1] - q0) : 0;
+  s.len = min(n, c.max_pages * c.page_size);
   s.items = (s.nq * H + kCols - 1) / kCols;
   // step is 16, 32, 64 or 128
   s.steps = (s.len + step - 1) >> (31 - __builtin_clz(step));
@@ -130,6 +134,7 @@ __device__ __forceinline__ SeqWork seq_lane(const SeqWork& s, int k) {
   SeqWork r;
   r.q0 = __builtin_amdgcn_readlane(s.q0, k);
   r.nq = __builtin_amdgcn_readlane(s.nq, k);
+  r.first = __builtin_amdgcn_readlane(s.first, k);
   r.len = __builtin_amdgcn_readlane(s.len, k);
   r.items = __builtin_amdgcn_readlane(s.items, k);
   r.steps = __builtin_amdgcn_readlane(s.steps, k);
@@ -159,7 +164,7 @@ struct WorkMap {
       if (lane == 0) lo = before;
     }
     end = __builtin_amdgcn_readlane(hi, 63);
-    s = SeqWork{0, 0, 0, 0, 0};
+    s = SeqWork{0, 0, 0, 0, 0, 0};
     if (b < c.n_seq) s = seq_work(c, b, lo, hi - lo, H, step);
     ws = s.items * s.steps, is = s.items;
     if (c.n_seq > 1) {
@@ -383,7 +388,7 @@ __global__ void __launch_bounds__(64) absorb_kernel(LatentAttnArgs a, char* qout
     WorkMap map{c, a.T, a.H, 32, lane};
     SeqWork s;
     int sb, ib;
-    if (map.find(false, t, s, sb, ib) >= 0) pos = max(0, s.len - s.nq + (t - s.q0));
+    if (map.find(false, t, s, sb, ib) >= 0) pos = max(0, s.first + (t - s.q0));
   }
   float f = 1.0f;  // of head h0 + lane / 8
   if constexpr (CD == kDtF16) {
@@ -591,9 +596,8 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
     const int rows = sw.nq * a.H;
     const int rr = min(ml_, rows - 1 - item * kCols);  // within the item
     const int64_t m0 = static_cast<int64_t>(sw.q0) * a.H + item * kCols;
-    const int first = sw.len - sw.nq;  // position of the sequence's first query
-    const int pos = first + quotient(item * kCols + rr, a.heads);
-    const int pos_min = first + quotient(item * kCols, a.heads);
+    const int pos = sw.first + quotient(item * kCols + rr, a.heads);
+    const int pos_min = sw.first + quotient(item * kCols, a.heads);
     const float qs = a.qsc[m0 + rr];
     // (piece of 16 bytes: slice k of 16 columns, the lane's half of it, part f of an fp32 eight)
     const char* qbase = a.q + q_offset<CD, TQ>(m0 + rr, 0, 32 * u0 + 8 * hh, c.row);

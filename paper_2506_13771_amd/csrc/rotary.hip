@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kRThreads) append_kernel(AppendArgs a, bool ve
       break;
     }
   }
-  if (b < 0 || c.cu[b] > t) return;
+  if (b < 0 || c.cu[0] > t) return;
   const int64_t pos = static_cast<int64_t>(c.lens[b]) - (static_cast<int64_t>(c.cu[b + 1]) - t);
   if (pos < 0 || pos >= static_cast<int64_t>(c.max_pages) * c.page_size) return;
   const int pg = static_cast<int>(pos) / c.page_size, off = static_cast<int>(pos) - pg * c.page_size;

@@ -136,3 +136,74 @@ def test_queries_before_the_first_token_stay_0():
     paths, _ = _layer(g, r, H * (dn + dv))
     out = lb.lb_latent_attention(_normal(g, 4, H, dn).cuda(), P.cache, paths, H, dv, *P.meta)
     assert bool((out[:2] == 0).all()) and bool(torch.isnan(out[2:]).all())
+
+
+# ----------------------------------------------------------------------------
+# lengths past the page table
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("act,cd", [("f32", "f32"), ("bf16", "bf16")])
+def test_append_and_attention_agree_past_the_table(act, cd):
+    # sequence 0's length passes its table by 2 (three new tokens, one of which has a place), sequence 1 is full, the
+    # third one's prefix sum passes the call's rows by 5
+    H, dn, dv, r, dr, page, M = 4, 32, 32, 24, 16, 8, 6
+    cap, news, g = M * page, [3, 2, 4], _gen(91)
+    lens = [cap + 2, cap, 30]
+    T, cu = sum(news), [0, 3, 5, 14]  # nine rows
+    data = torch.zeros((3 * M, page, lb.lb_latent_row(r, dr)), dtype=DT[cd])
+    table = torch.randperm(3 * M, generator=g).int().view(3, M)
+    rows = _normal(g, 3, cap, 2 * r + dr, dtype=cd)
+    for b in range(3):
+        for t in range(cap):
+            data[table[b, t // page], t % page, :2 * r + dr] = rows[b, t]
+    f = _freqs(dr)
+    w, kr = _normal(g, T, 2, r, dtype=act), _normal(g, T, dr, dtype=act)
+    cache = lb.LatentCache(data.cuda(), r, dr)
+    meta = (table.cuda(), _ints(lens).cuda(), _ints(cu).cuda())
+    lb.lb_latent_append(cache, w.cuda(), kr.cuda(), f.cuda(), *meta)
+    got = cache.data.cpu()
+    place = []  # (sequence, position) of each row
+    for b, (lo, hi) in enumerate(((0, 3), (3, 5), (5, 9))):
+        place += [(b, lens[b] - (cu[b + 1] - t)) for t in range(lo, hi)]
+    kept = torch.ones(got.shape[:2], dtype=torch.bool)
+    for t, (b, pos) in enumerate(place):
+        if pos < cap:
+            at = (int(table[b, pos // page]), pos % page)
+            kept[at] = False
+            turned = R.turn(kr[t:t + 1].double(), _ints([pos]), f)
+            _within(got[at][2 * r:2 * r + dr][None], turned, R.turn_bound(kr[t:t + 1].double(), DT[cd]) + R.small(DT[cd]), t)
+            rows[b, pos] = got[at][:2 * r + dr]
+    assert torch.equal(_bits(got[kept]), _bits(data[kept]))
+    paths, up = _layer(g, r, H * (dn + dv))
+    q = _normal(g, T, H, dn + dr, dtype=act)
+    out = lb.lb_latent_attention(q.cuda(), cache, paths, H, dv, *meta, f.cuda())
+    for t, (b, pos) in enumerate(place):
+        qt = torch.cat([q[t:t + 1, :, :dn].double(), R.turn(q[t:t + 1, :, dn:].double(), _ints([pos]), f)], -1)
+        n = min(pos + 1, cap)
+        ref, bound = _turned_reference(qt, q[t:t + 1], rows[b, :n].double(), up, H, dv, n, dr, (dn + dr) ** -0.5, DT[cd])
+        _within(out[t:t + 1], ref, bound, (t, b, pos))
+
+
+def test_lengths_below_zero_and_at_the_end_of_32_bits():
+    H, dn, dv, r, page = 2, 16, 16, 16, 8
+    g = _gen(92)
+    P = Paged(g, [20, 20, 20], [2, 2, 2], r, 0, page, "f32")
+    P.table[2] = P.table[2, 0]  # every place has a page
+    paths, up = _layer(g, r, H * (dn + dv))
+    q = _normal(g, 6, H, dn)
+    lens = [-(2 ** 31), 20, 2 ** 31 - 1]
+    meta = (P.table.cuda(), _ints(lens).cuda(), P.meta[2])
+    before = P.cache.data.clone()
+    lb.lb_latent_append(P.cache, _normal(g, 6, 2, r).cuda(), None, None, *meta)
+    changed = (_bits(P.cache.data) != _bits(before)).any(-1).cpu()
+    assert int(changed.sum()) == 2 and all(bool(changed[int(P.table[1, t // page]), t % page]) for t in (18, 19))
+    P.rows[1][18:] = torch.stack([P.cache.data[int(P.table[1, t // page]), t % page].cpu()[:2 * r] for t in (18, 19)]).double()
+    out = lb.lb_latent_attention(q.cuda(), P.cache, paths, H, dv, *meta)
+    assert bool((out[:2] == 0).all())
+    ref, bound = R.latent_attention(q[2:4], [P.rows[1]], up, H, dv, [20], [2], None, 0, dn ** -0.5, torch.float32)
+    _within(out[2:4], ref, bound, "the sequence between them")
+    # all places are seen
+    n = P.table.shape[1] * page
+    one = P.cache.data[int(P.table[2, 0])].cpu()[:, :2 * r].double().repeat(P.table.shape[1], 1)
+    for t in (4, 5):
+        ref, bound = R.latent_attention(q[t:t + 1], [one], up, H, dv, [n], [1], None, 0, dn ** -0.5, torch.float32)
+        _within(out[t:t + 1], ref, bound, "a length past every table")
