@@ -280,7 +280,8 @@ size_t lb_attention_backward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t H, 
   if (Tq < 0 || Tk < 0 || H < 0 || Hk < 1 || H % Hk != 0 || d_rope < 0 || d_rope > 192 || !fits(Tq, H) ||
       !fits(Tk, Hk, d_rope))
     return 0;
-  return 256 + up256(Tq * H * 4) + up256(Tk * Hk * d_rope * 4);
+  const size_t n = up256(Tq * H * 4) + up256(Tk * Hk * d_rope * 4);
+  return n > 0 ? n : 256;
 }
 
 lb_status lb_attention_backward(const lb_attention* a, const void* o, const float* lse, const void* d_o,
@@ -314,9 +315,8 @@ lb_status lb_attention_backward(const lb_attention* a, const void* o, const floa
   r.dq = grads->dq, r.dk = grads->dk, r.dv = grads->dv, r.dkr = grads->dk_rope;
   r.dk_t = grads->dk_t, r.dk_h = grads->dk_h, r.dv_t = grads->dv_t, r.dv_h = grads->dv_h;
   char* ws = static_cast<char*>(workspace);
-  r.top = reinterpret_cast<float*>(ws);
-  r.delta = reinterpret_cast<float*>(ws + 256);
-  r.dkr_part = reinterpret_cast<float*>(ws + 256 + up256(a->Tq * a->H * 4));
+  r.delta = reinterpret_cast<float*>(ws);
+  r.dkr_part = reinterpret_cast<float*>(ws + up256(a->Tq * a->H * 4));
   return hip_status(lb::launch_attn_backward(r, stream));
 }
 

@@ -39,27 +39,41 @@ struct BwdArgs {
   int qvec, kvec, vvec;  // dq, dk, dv rows may be written four elements at a time
 };
 
-// f16: dS is brought to f16's normal range by a power of two of the largest |dO|
-// (products of small gradients and small probabilities would fall below it)
-template <int DT>
-__device__ __forceinline__ float ds_factor(const float* top) {
-  if constexpr (DT != kDtF16) return 1.0f;
-  const float t = *top;
-  if (!(t > 0.0f) || t > 1e30f) return 1.0f;
-  int ex;
-  frexpf(t, &ex);
-  return ldexpf(1.0f, 4 - ex);  // the largest |dO| to [8, 16)
-}
-
-// The largest |dO| (f16 only; a maximum: its order does not matter)
-__global__ void __launch_bounds__(kThreads) top_kernel(const uint16_t* d_o, int64_t n, float* top) {
-  float t = 0.0f;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * kThreads)
-    t = fmaxf(t, fabsf(f16_bits_to_f32(d_o[i])));
+// f16: dS (|dO| |V| times a probability: anything from 2^-60 to 2^40) enters its products times a
+// power of two, kept for each column of the accumulators (a query in one kernel, a key in the
+// other) and lowered once the column's largest value passes 2^15, which brings it to 2^11 .. 2^12; the
+// column's sums follow.  A value then keeps its 11 bits down to 2^-25 of the column's largest, whatever other
+// columns, sequences or rows behind the last sequence hold.
+constexpr float kDsMost = 32768.0f;
+constexpr float kDsStart = 1.152921504606846976e18f;  // 2^60: what it leaves too small is far below f16's results
+template <int DT, int T>
+__device__ __forceinline__ void scale_ds(floatx16& ds, float& fac, floatx16 (&acc)[T]) {
+  if constexpr (DT == kDtF16) {
+    float m = 0.0f;
 #pragma unroll
-  for (int m = 32; m > 0; m >>= 1) t = fmaxf(t, __shfl_xor(t, m));
-  if ((threadIdx.x & 63) == 0 && t > 0.0f)
-    __hip_atomic_fetch_max(reinterpret_cast<uint32_t*>(top), __float_as_uint(t), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(ds[e]));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    if (__any(m * fac > kDsMost)) {
+      float to = fac;
+      if (m * fac > kDsMost) {
+        int ex;
+        frexpf(fminf(m, 1e30f), &ex);
+        to = ldexpf(1.0f, 12 - ex);
+      }
+      const float r = to / fac;
+      fac = to;
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t][e] *= r;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) ds[e] *= fac;
+  }
+}
+template <int DT>
+constexpr float ds_start() {
+  return DT == kDtF16 ? kDsStart : 1.0f;
 }
 
 // S and dO V^T of a 32 x 32 block: A operands from rows of the tiles t0 (KC slices) and
@@ -205,7 +219,6 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   const int n_end = a.causal ? min(nk, min(i0 + kBM, nq) + off) : nk;
   const int w_end = a.causal ? min(n_end, i0 + w0 + 32 + off) : n_end;
   const float sc = a.scale * kLog2e;
-  const float fac = ds_factor<DT>(a.top);
 
   const char* kp = static_cast<const char*>(a.k) + (k_lo * a.k_t + kvh * a.k_h) * ES;
   const char* vp = static_cast<const char*>(a.v) + (k_lo * a.v_t + kvh * a.v_h) * ES;
@@ -328,16 +341,19 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) gq[t][e] = 0.0f;
+  float fac = ds_start<DT>();
   walk(false, [&](const char* kt, const char* vt, int r0, int j, auto&& between) __attribute__((always_inline)) {
     floatx16 s, dp;
     scores<DT, KC, 2 * VT, BN, SG>(kt, vt, r0, lane, qf, df, s, dp, between);
     probabilities(j, s);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) dp[e] = s[e] == 0.0f ? 0.0f : s[e] * (dp[e] - del) * fac;
+    for (int e = 0; e < 16; ++e) dp[e] = s[e] == 0.0f ? 0.0f : s[e] * (dp[e] - del);
+    scale_ds<DT>(dp, fac, gq);
     add_products<DT, KT, BN, SG, DST>(kt, r0, lane, dp, gq);
   });
   if constexpr (SPREAD) wait_loads();  // none may arrive after the workgroup's end
-  const float qs = a.scale / fac;
+  // (the waves' parts have factors of their own)
+  const float inv = 1.0f / fac, qs = WIDE ? a.scale * inv : a.scale;
   char* gp = static_cast<char*>(a.dq) + row * dk * ES;
 #pragma unroll
   for (int n = 0; n < KT; ++n) {
@@ -350,6 +366,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
       }
     } else {
       float v[4];
+      if constexpr (DT == kDtF16) gq[n] *= inv;
       join_waves(reinterpret_cast<float*>(smem), gq[n], wave, lane, v);
       if (i < nq) store4<DT>(gp, 32 * n + 8 * wave + 4 * hh, dk, f.qvec, v[0] * qs, v[1] * qs, v[2] * qs, v[3] * qs);
     }
@@ -379,7 +396,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
   const int j0 = tile * kBM, j = j0 + w0 + col;                    // this lane's key
   const int dk = a.d_nope + a.d_rope, dv = a.d_v;
   const float sc = a.scale * kLog2e;
-  const float fac = ds_factor<DT>(a.top);
 
   const int i_begin = a.causal ? max(0, j0 - off) / BQ * BQ : 0;
   const int n_it = max(0, (nq - i_begin + BQ - 1) / BQ), total = G * n_it;
@@ -442,6 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) gv[t][e] = 0.0f;
 
+  float fac = ds_start<DT>();
   int i_now = i_begin, g_now = 0;
   for (int it = 0; it < total; ++it) {
     char* qt = smem + (WIDE ? (it & 1) * TB : 0);
@@ -483,15 +500,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
           float p = exp2_fast(s[e + q] * sc - lv[q]);
           if (mask && i_here + row + q + off < j) p = 0.0f;
           s[e + q] = p;
-          dp[e + q] = p == 0.0f ? 0.0f : p * (dp[e + q] - dl[q]) * fac;
+          dp[e + q] = p == 0.0f ? 0.0f : p * (dp[e + q] - dl[q]);
         }
       }
       add_products<DT, VT, BQ>(dt, rb + 32 * b, lane, s, gv);
+      scale_ds<DT>(dp, fac, gk);
       add_products<DT, KT, BQ>(qt, rb + 32 * b, lane, dp, gk);
     }
   }
   const int64_t t = k_lo + min(j, nk - 1);
-  const float ks = a.scale / fac;
+  const float inv = 1.0f / fac, ks = WIDE ? a.scale * inv : a.scale;
   char* gkp = static_cast<char*>(a.dk) + (t * a.dk_t + kvh * a.dk_h) * ES;
   char* gvp = static_cast<char*>(a.dv) + (t * a.dv_t + kvh * a.dv_h) * ES;
   float* grp = a.dkr_part + (static_cast<int64_t>(kvh) * a.Tk + t) * a.d_rope;
@@ -525,6 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
       for (int e = 0; e < 16; e += 4) put_k(32 * n + 2 * e + 4 * hh, gk[n][e], gk[n][e + 1], gk[n][e + 2], gk[n][e + 3]);
     } else {
       float v[4];
+      if constexpr (DT == kDtF16) gk[n] *= inv;
       join_waves(buf, gk[n], wave, lane, v);
       put_k(32 * n + 8 * wave + 4 * hh, v[0], v[1], v[2], v[3]);
     }
@@ -601,20 +620,7 @@ hipError_t bwd_kc(const BwdArgs& f, hipStream_t stream) {
 }
 template <int DT>
 hipError_t bwd_dt(const BwdArgs& f, hipStream_t stream) {
-  const AttnArgs& a = f.a;
-  if constexpr (DT == kDtF16) {
-    hipError_t e = launch_zero_elems(a.top, 1, kDtF32, stream);
-    if (e != hipSuccess) return e;
-    const int64_t n = static_cast<int64_t>(a.Tq) * a.H * a.d_v;
-    if (n > 0) {
-      const int64_t blocks = (n + 8 * kThreads - 1) / (8 * kThreads);
-      hipLaunchKernelGGL(top_kernel, dim3(static_cast<uint32_t>(blocks < 2048 ? blocks : 2048)), dim3(kThreads), 0, stream,
-                         static_cast<const uint16_t*>(a.d_o), n, a.top);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
-  }
-  return a.d_v <= 64 ? bwd_kc<DT, 2>(f, stream) : bwd_kc<DT, 4>(f, stream);
+  return f.a.d_v <= 64 ? bwd_kc<DT, 2>(f, stream) : bwd_kc<DT, 4>(f, stream);
 }
 
 }  // namespace

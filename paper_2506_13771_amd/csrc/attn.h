@@ -72,7 +72,6 @@ struct AttnArgs {
   void *dq, *dk, *dv, *dkr;
   int64_t dk_t, dk_h, dv_t, dv_h;
   float* delta;     // [Tq][H]: rowsum(dO (.) O)
-  float* top;       // the largest |dO| (16-bit floats)
   float* dkr_part;  // [Hk][Tk][d_rope]
 };
 

@@ -207,3 +207,105 @@ def test_lengths_below_zero_and_at_the_end_of_32_bits():
     for t in (4, 5):
         ref, bound = R.latent_attention(q[t:t + 1], [one], up, H, dv, [n], [1], None, 0, dn ** -0.5, torch.float32)
         _within(out[t:t + 1], ref, bound, "a length past every table")
+
+
+# ----------------------------------------------------------------------------
+# gradients of f16 heads
+# ----------------------------------------------------------------------------
+def _f16_gradients(q, k, v, lens_q, lens_k, causal, do, groups=1):
+    """dq, dk, dv (fp64) with bounds, of attention without a rotary key.  As attn_ref's, but for dS's smallest step: a
+    power of two brings each query's (for dq) and each key's (for dk) largest |dS| to 2^11 or more, so that what lies
+    below f16's normal range is off by 2^-25 of 2^-11 of that largest value."""
+    H, Hk, d, dv_ = q.shape[1], k.shape[1], q.shape[2], v.shape[2]
+    z = lambda *s: torch.zeros(s, dtype=torch.float64)  # noqa: E731
+    r = dict(dq=z(*q.shape), dk=z(*k.shape), dv=z(*v.shape))
+    r.update({n + "_b": torch.zeros_like(x) for n, x in list(r.items())})
+    u, e32, scale, step = R.HALF[torch.float16], R.E32, d ** -0.5, 2.0 ** -36
+    a = b = 0
+    for n, m in zip(lens_q, lens_k):
+        seen = R.seen_mask(n, m, causal)
+        for g in range(Hk):
+            heads = range(g * H // Hk, (g + 1) * H // Hk)
+            parts = []
+            for h in heads:
+                x = do[a:a + n, h].double()
+                hd = R.Head(q[a:a + n, h].double(), k[b:b + m, g].double(), v[b:b + m, g].double(), seen, scale, torch.float16)
+                dp = x @ hd.v.T
+                dd = (x * hd.o).sum(-1, keepdim=True)
+                ds = hd.p * (dp - dd)
+                e_dp = (dv_ + 4) * e32 * (x.abs() @ hd.v.abs().T)
+                e_d = (x.abs() * (hd.o_bound + dv_ * e32 * hd.o.abs())).sum(-1, keepdim=True)
+                e_ds = hd.p * (e_dp + e_d) + ds.abs() * (u + 2 * hd.es[:, None] + 8 * e32)
+                top = ds.abs().amax(1, keepdim=True)
+                r["dq"][a:a + n, h] = ds @ hd.k * scale
+                r["dq_b"][a:a + n, h] = ((e_ds + step * top) @ hd.k.abs() + (m + 4) * e32 * (ds.abs() @ hd.k.abs())) * scale
+                r["dv"][b:b + m, g] += hd.p.T @ x
+                r["dv_b"][b:b + m, g] += (hd.p * hd.up[:, None] + R.small(torch.float16) * (hd.p > 0)).T @ x.abs() + (
+                    n + 4) * e32 * (hd.p.T @ x.abs())
+                parts.append((hd.q, ds, e_ds))
+            top = torch.stack([p[1].abs().amax(0) for p in parts]).amax(0)
+            for qq, ds, e_ds in parts:
+                r["dk"][b:b + m, g] += ds.T @ qq * scale
+                r["dk_b"][b:b + m, g] += ((e_ds + step * top).T @ qq.abs() + (len(parts) * n + 4) * e32 * (ds.abs().T @ qq.abs())) * scale
+        a, b = a + n, b + m
+    for n in ("dq", "dk", "dv"):
+        r[n + "_b"] += u * r[n].abs() + R.small(torch.float16)
+    return r
+
+
+def _run_f16(q, k, v, lens_q, lens_k, causal, do, pad=0, fill=0.0):
+    """lb's gradients, with `pad` rows behind the last sequence that hold `fill`."""
+    p = lambda x: torch.cat([x, torch.full((pad,) + x.shape[1:], fill, dtype=x.dtype)]).cuda()  # noqa: E731
+    args = [p(x) for x in (q, k, v)] + [None]
+    cu = (_cum(lens_q).cuda(), _cum(lens_k).cuda())
+    o, lse = lb.lb_attention_forward(*args, *cu, causal=causal)
+    o[sum(lens_q):], lse[sum(lens_q):] = fill, fill
+    got = lb.lb_attention_backward(*args, o, lse, p(do), *cu, causal=causal)
+    return dict(dq=got[0][:q.shape[0]], dk=got[1][:k.shape[0]], dv=got[2][:v.shape[0]])
+
+
+def _agree(got, ref, what):
+    for n in ("dq", "dk", "dv"):
+        a, x, b = got[n].cpu().double(), ref[n], ref[n + "_b"]
+        # (a value past f16's largest is an infinity of its sign; next to it, either)
+        over, near = x.abs() - b >= 65520, x.abs() + b >= 65504
+        assert bool((a[over] == x[over].sign() * math.inf).all()), (what, n)
+        _within(torch.where(near, torch.zeros_like(a), a), torch.where(near, torch.zeros_like(x), x), b, (what, n))
+
+
+@pytest.mark.parametrize("fill", [6e4, 100.0, math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("H", [2, 48])
+def test_f16_gradients_beside_padding(fill, H):
+    # rows behind the last sequence hold anything
+    lens, d, g = [130, 470], 64, _gen(4)
+    q, k, v = (_normal(g, 600, H, d, dtype="f16") for _ in range(3))
+    do = _normal(g, 600, H, d, dtype="f16", std=1e-3)
+    ref = _f16_gradients(q, k, v, lens, lens, False, do)
+    _agree(_run_f16(q, k, v, lens, lens, False, do, 5, fill), ref, fill)
+
+
+@pytest.mark.parametrize("d,dv", [(64, 128), (128, 64), (192, 128)])
+@pytest.mark.parametrize("size,do_size", [(130.0, 1.0), (128.0, 1e-4), (60000.0, 4.0)])
+@pytest.mark.parametrize("H", [1, 200])
+def test_f16_gradients_of_large_values(d, dv, size, do_size, H):
+    # equal scores of two keys with opposite values aligned with dO: dS reaches half of |dO| |V| dv
+    n = 130 if H > 1 else 2
+    g = _gen(5)
+    q, k = _normal(g, n, H, d, dtype="f16", std=1e-3), _normal(g, 2, H, d, dtype="f16", std=1e-3)
+    v = (torch.ones(2, H, dv) * torch.tensor([1.0, -1.0]).view(2, 1, 1) * size).half()
+    do = torch.full((n, H, dv), do_size).half()
+    ref = _f16_gradients(q, k, v, [n], [2], False, do)
+    _agree(_run_f16(q, k, v, [n], [2], False, do), ref, (d, dv, size))
+
+
+@pytest.mark.parametrize("H,Hk", [(2, 2), (4, 1), (64, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_f16_gradients_beside_one_large_one(H, Hk, causal):
+    # one token's gradient 10^7 times the others': theirs keep their digits
+    lens, d, g = [300, 200], 64, _gen(6)
+    q, k, v = _normal(g, 500, H, d, dtype="f16"), _normal(g, 500, Hk, d, dtype="f16"), _normal(g, 500, Hk, d, dtype="f16")
+    do = _normal(g, 500, H, d, dtype="f16", std=1e-3)
+    do[7] *= 1e7
+    assert bool(torch.isfinite(do).all())
+    ref = _f16_gradients(q, k, v, lens, lens, causal, do)
+    _agree(_run_f16(q, k, v, lens, lens, causal, do), ref, (H, Hk, causal))
