@@ -71,6 +71,16 @@ __device__ __forceinline__ void scale_ds(floatx16& ds, float& fac, floatx16 (&ac
     for (int e = 0; e < 16; ++e) ds[e] *= fac;
   }
 }
+// f16: P enters dV's product times 2^14, so that it keeps its 11 bits down to 2^-28 (a key that every
+// query gives little has its gradient from nothing else); dS has the factor too
+template <int DT>
+constexpr float p_bits() {
+  return DT == kDtF16 ? 14.0f : 0.0f;
+}
+template <int DT>
+constexpr float p_factor() {
+  return DT == kDtF16 ? 1.0f / 16384.0f : 1.0f;
+}
 template <int DT>
 constexpr float ds_start() {
   return DT == kDtF16 ? kDsStart : 1.0f;
@@ -422,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
       // rows past the end and rows that see no key get probability 0
       const bool ok = i0 + tid < nq && lr != -INFINITY;
       float* st = reinterpret_cast<float*>(t + TB - 8 * BQ);
-      st[tid] = ok ? lr * kLog2e : INFINITY, st[BQ + tid] = ok ? de : 0.0f;
+      st[tid] = ok ? lr * kLog2e - p_bits<DT>() : INFINITY, st[BQ + tid] = ok ? de : 0.0f;
     }
   };
   auto next = [&](int& i0, int& g) {
@@ -509,12 +519,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_keys(BwdArgs f) {
     }
   }
   const int64_t t = k_lo + min(j, nk - 1);
-  const float inv = 1.0f / fac, ks = WIDE ? a.scale * inv : a.scale;
+  const float inv = p_factor<DT>() / fac, ks = WIDE ? a.scale * inv : a.scale;
   char* gkp = static_cast<char*>(a.dk) + (t * a.dk_t + kvh * a.dk_h) * ES;
   char* gvp = static_cast<char*>(a.dv) + (t * a.dv_t + kvh * a.dv_h) * ES;
   float* grp = a.dkr_part + (static_cast<int64_t>(kvh) * a.Tk + t) * a.d_rope;
   auto put_v = [&](int c, float v0, float v1, float v2, float v3) {
-    if (j < nk) store4<DT>(gvp, c, dv, f.vvec, v0, v1, v2, v3);
+    constexpr float u = p_factor<DT>();
+    if (j < nk) store4<DT>(gvp, c, dv, f.vvec, v0 * u, v1 * u, v2 * u, v3 * u);
   };
   auto put_k = [&](int c, float v0, float v1, float v2, float v3) {
     if (j >= nk) return;

@@ -309,3 +309,29 @@ def test_f16_gradients_beside_one_large_one(H, Hk, causal):
     assert bool(torch.isfinite(do).all())
     ref = _f16_gradients(q, k, v, lens, lens, causal, do)
     _agree(_run_f16(q, k, v, lens, lens, causal, do), ref, (H, Hk, causal))
+
+
+# ----------------------------------------------------------------------------
+# small probabilities in f16
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("H", [2, 130])
+@pytest.mark.parametrize("grad", [1.0, 1000.0])
+def test_f16_values_gradient_of_little_seen_keys(H, grad):
+    # keys that every query gives 2^-12 to 2^-27 of its weight; their dV comes from such probabilities alone
+    n, m, d, dv, g = 600, 128, 8, 64, _gen(9)
+    k = torch.zeros(m, H, d, dtype=torch.float16)
+    k[1:, :, 0] = -torch.linspace(12.0, 27.0, m - 1)[:, None].half()
+    q = torch.zeros(n, H, d, dtype=torch.float16)
+    q[..., 0] = math.log(2.0)
+    v = _normal(g, m, H, dv, dtype="f16")
+    do = _normal(g, n, H, dv, dtype="f16", std=grad)
+    args = [t.cuda() for t in (q, k, v)] + [None]
+    o, lse = lb.lb_attention_forward(*args, causal=False, scale=1.0)
+    got = lb.lb_attention_backward(*args, o, lse, do.cuda(), causal=False, scale=1.0)[2]
+    for h in (0, H - 1):
+        hd = R.Head(q[:, h].double(), k[:, h].double(), v[:, h].double(), R.seen_mask(n, m, False), 1.0, torch.float16)
+        ref = hd.p.T @ do[:, h].double()
+        # as attn_ref's bound, with f16's smallest step 2^-14 of what it is there
+        bound = (hd.p * hd.up[:, None] + 2.0 ** -14 * R.small(torch.float16)).T @ do[:, h].double().abs() + (
+            n + 4) * R.E32 * (hd.p.T @ do[:, h].double().abs()) + R.HALF[torch.float16] * ref.abs() + R.small(torch.float16)
+        _within(got[:, h], ref, bound, (H, h))
