@@ -528,7 +528,8 @@ lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const vo
    multiple of Hk; d_nope, d_v <= 256; T H < 2^22; (T H / 32 + n_seq) (max_pages page_size / 16
    + 1) < 2^31 (LB_ERR_SHAPE); scale finite and > 0
    (LB_ERR_ARG).  q' enters the scores with at least 16 significant bits (24 for
-   fp32 activations), softmax statistics and sums are fp32; probabilities enter
+   fp32 activations; over an f16 cache 22 of values down to 2^-17, and 16 down to 2^-22, of the larger of
+   d_nope max |h q| and 1.5 max |q[d_nope ..]| of its row), softmax statistics and sums are fp32; probabilities enter
    the sums rounded to the cache's type where out's is no finer, else in two or
    three terms of it (22 bits or more for fp32 activations).  A NaN or infinity in
    the row of a new token may reach the call's earlier queries of its sequence,

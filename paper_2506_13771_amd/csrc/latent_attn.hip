@@ -274,15 +274,16 @@ __device__ __forceinline__ int64_t q_offset(int64_t m, int n, int col, int row) 
   return (((m >> 5) * TQ + n) * (row / EP) + col / EP) * 512 + (m & 31) * 16 + col % EP * esize<CD>();
 }
 
-// With an f16 cache q' is brought into f16's range by a power of two per row: the
-// inverse of a bound on the row's values (order-free maxima, so that every workgroup
-// finds the same one).  top: the largest |h (.) q|, rope: of the rotary part.
+// With an f16 cache q' is brought into f16's range by a power of two per row, which takes a
+// bound on the row's values (order-free maxima, so that every workgroup finds the same one) to
+// 2^13 .. 2^14: two terms then hold 22 bits of values down to 2^-17 of the bound and 16 down to 2^-23, so
+// that a small rotary part beside large latents keeps its digits.  top: the largest |h (.) q|, rope: of the rotary part.
 __device__ __forceinline__ float row_factor(float top, float rope, int dn) {
   const float b = fmaxf(top * static_cast<float>(dn), 1.5f * rope);
   if (!(b > 0.0f) || b > 1e38f) return 1.0f;
   int ex;
   frexpf(b, &ex);
-  return ldexpf(1.0f, max(-120, min(120, -ex)));
+  return ldexpf(1.0f, max(-120, min(120, 14 - ex)));
 }
 
 // The first H 2 nkb tiles workgroups (a wave each) take 32 latents of a path (one packed

@@ -335,3 +335,44 @@ def test_f16_values_gradient_of_little_seen_keys(H, grad):
         bound = (hd.p * hd.up[:, None] + 2.0 ** -14 * R.small(torch.float16)).T @ do[:, h].double().abs() + (
             n + 4) * R.E32 * (hd.p.T @ do[:, h].double().abs()) + R.HALF[torch.float16] * ref.abs() + R.small(torch.float16)
         _within(got[:, h], ref, bound, (H, h))
+
+
+# ----------------------------------------------------------------------------
+# an f16 cache: parts of a query that differ much in size
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("act", ["f32", "f16"])
+@pytest.mark.parametrize("large", ["latents", "rotary"])
+def test_f16_cache_keeps_the_smaller_part_of_a_query(act, large):
+    # |h q| of thousands beside a rotary part near 1 (or the reverse), while the cache holds the smaller part's
+    # counterparts some thousand times larger: both parts decide the scores
+    n, H, dn, dv, r, dr, page, g = 200, 3, 128, 32, 64, 64, 16, _gen(61)
+    w = _normal(g, n, 2 * r + dr)
+    up_w, up_q = (2.0 ** -11, 2.0 ** 13) if large == "latents" else (16.0, 2.0 ** -5)
+    w[:, :2 * r] *= up_w
+    w[:, 2 * r:] *= 4.0 if large == "latents" else 2.0 ** -9
+    w = w.half()
+    q = _normal(g, 1, H, dn + dr)
+    q[..., :dn] *= up_q
+    q[..., dn:] *= 1.0 if large == "latents" else 2.0 ** 11
+    q = q.to(DT[act])
+    paths, up = _layer(g, r, H * (dn + dv))
+    data = torch.zeros(-(-n // page), page, lb.lb_latent_row(r, dr), dtype=torch.float16)
+    data.view(-1, data.shape[-1])[:n, :2 * r + dr] = w
+    f, scale = _freqs(dr), (dn + dr) ** -0.5
+    out = lb.lb_latent_attention(q.cuda(), lb.LatentCache(data.cuda(), r, dr), paths, H, dv,
+                                 torch.arange(data.shape[0], dtype=torch.int32).view(1, -1).cuda(), _ints([n]).cuda(),
+                                 _ints([0, 1]).cuda(), f.cuda())
+    rows = w.double()
+    ref, bound = R.latent_attention(q, [rows], up, H, dv, [n], [1], f, dr, scale, torch.float32)
+    # attn_ref's bound with q' as fp32 holds it, and for the two f16 terms 2^-22 of every element (all are above 2^-17
+    # of the row's bound but for those near 0: 2^-25 2^-13 of it), for a probability 2^-22, or 2^-11 (f16 activations)
+    for h in range(H):
+        uk, v = up[:, h * dn:(h + 1) * dn], rows[:, :2 * r] @ up[:, H * dn + h * dv:H * dn + (h + 1) * dv]
+        x = q[0, h].double()
+        qa = torch.cat([uk @ x[:dn], R.turn(x[None, dn:], _ints([n - 1]), f)[0]])
+        top = max(dn * float((up.abs().amax() * x[:dn].abs()).max()), 1.5 * float(x[dn:].abs().max()))
+        e = scale * float((rows.abs() @ (2.0 ** -22 * qa.abs() + 2.0 ** -38 * top)).max())
+        p = torch.softmax(rows @ qa * scale, 0)
+        bound[0, h] += (2 * e + (2.0 ** -22 if act == "f32" else 2.0 ** -11)) * (p @ v.abs()) + 2.0 ** -25 * v.abs().sum(0)
+        assert 0.1 < float((rows[:, :2 * r] @ qa[:2 * r]).std() * scale) < 30 and 0.1 < float((rows[:, 2 * r:] @ qa[2 * r:]).std() * scale) < 30
+    _within(out, ref, bound, (act, large))
