@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kThreads, DT == kDtF32 || !WIDE ? 1 : 2) attn_
   const float inv = mx == -INFINITY ? 0.0f : 1.0f / sum;
   const int64_t row = static_cast<int64_t>(q_lo + i) * a.H + h;
   if (a.lse != nullptr && hh == 0 && (WIDE || wave == 0))
-    a.lse[row] = mx == -INFINITY ? -INFINITY : mx * a.scale + log2f(sum) * kLn2;
+    a.lse[row] = mx * a.scale + log2f(sum) * kLn2;  // (no key: -infinity twice; scores all NaN: sum is)
   char* op = static_cast<char*>(a.o) + row * dv * ES;
 #pragma unroll
   for (int t = 0; t < VT; ++t)

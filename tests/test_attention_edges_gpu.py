@@ -376,3 +376,26 @@ def test_f16_cache_keeps_the_smaller_part_of_a_query(act, large):
         bound[0, h] += (2 * e + (2.0 ** -22 if act == "f32" else 2.0 ** -11)) * (p @ v.abs()) + 2.0 ** -25 * v.abs().sum(0)
         assert 0.1 < float((rows[:, :2 * r] @ qa[:2 * r]).std() * scale) < 30 and 0.1 < float((rows[:, 2 * r:] @ qa[2 * r:]).std() * scale) < 30
     _within(out, ref, bound, (act, large))
+
+
+# ----------------------------------------------------------------------------
+# NaN
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("H", [2, 300])
+def test_a_nan_query_is_not_taken_for_one_that_sees_nothing(dtype, H):
+    # o, lse and the gradients of a NaN query are NaN; a query without keys has lse -infinity, o and dq 0
+    lens_q, lens_k, d = [40, 30], [40, 28], 32
+    g = _gen(71)
+    q, k, v = _normal(g, 70, H, d, dtype=dtype), _normal(g, 68, H, d, dtype=dtype), _normal(g, 68, H, d, dtype=dtype)
+    q[5, 0] = math.nan
+    do = _normal(g, 70, H, d, dtype=dtype)
+    args, cu = [t.cuda() for t in (q, k, v)] + [None], (_cum(lens_q).cuda(), _cum(lens_k).cuda())
+    o, lse = lb.lb_attention_forward(*args, *cu)
+    assert bool(torch.isnan(o[5, 0]).all()) and bool(torch.isnan(lse[5, 0]))
+    assert bool((lse[40:42] == -math.inf).all()) and bool((o[40:42] == 0).all())
+    dq, dk, _, _ = lb.lb_attention_backward(*args, o, lse, do.cuda(), *cu)
+    assert bool(torch.isnan(dq[5, 0]).all()) and bool(torch.isnan(dk[:6, 0]).all()) and bool((dq[40:42] == 0).all())
+    fine = torch.ones(70, H, dtype=torch.bool)
+    fine[5, 0] = False
+    assert bool(torch.isfinite(o.cpu()[fine]).all()) and bool(torch.isfinite(dq.cpu()[fine]).all())
