@@ -498,7 +498,8 @@ int64_t lb_latent_row(int64_t r, int64_t d_rope);
      y_i = x_i cos a - x_{i+d/2} sin a,  y_{i+d/2} = x_{i+d/2} cos a + x_i sin a;
    inverse != 0 takes -a: the transposed map, which carries gradients back.
    Angles are formed in 64 bits, the products in fp32, rounded once.  Element
-   (t, h, i) of x is at t x_t + h x_h + i (strides in elements, >= 0), y alike;
+   (t, h, i) of x is at t x_t + h x_h + i (strides in elements, 0 to 2^40, with
+   (T - 1) x_t and (H - 1) x_h up to 2^59, here and in the calls below; LB_ERR_SHAPE), y alike;
    y's rows must not overlap each other (LB_ERR_ARG).  y may be x with the same
    strides; other overlaps of the spanned ranges are refused (LB_ERR_ARG).
    positions [T] int32, freqs [d / 2] fp32 (radians a position). */

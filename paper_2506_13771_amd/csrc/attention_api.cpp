@@ -31,9 +31,10 @@ constexpr int64_t kMaxRows = int64_t(1) << 22, kMaxGroups = int64_t(1) << 24;
 bool fits(int64_t a, int64_t b) { return a == 0 || b <= kMaxElems / a; }
 bool fits(int64_t a, int64_t b, int64_t c) { return fits(a, b) && fits(a * b, c); }
 
-// A strided [T x H x d] operand: its last element's offset within 2^62, strides >= 0
-constexpr int64_t kMaxStride = int64_t(1) << 40;
-bool strides_ok(int64_t st, int64_t sh) { return st >= 0 && sh >= 0 && st <= kMaxStride && sh <= kMaxStride; }
+// A strided [T x H x d] operand: strides >= 0, its last row at most twice kMaxOffset elements behind its first
+constexpr int64_t kMaxStride = int64_t(1) << 40, kMaxOffset = int64_t(1) << 59;
+bool stride_ok(int64_t n, int64_t s) { return s >= 0 && s <= kMaxStride && (n <= 1 || s <= kMaxOffset / (n - 1)); }
+bool strides_ok(int64_t T, int64_t H, int64_t st, int64_t sh) { return stride_ok(T, st) && stride_ok(H, sh); }
 // elements from the first to one past the last
 int64_t span(int64_t T, int64_t H, int64_t d, int64_t st, int64_t sh) { return (T - 1) * st + (H - 1) * sh + d; }
 // rows of d elements that share no element: heads inside tokens, or tokens inside heads
@@ -46,6 +47,11 @@ bool rows_apart(int64_t T, int64_t H, int64_t d, int64_t st, int64_t sh) {
 bool ranges_meet(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return na > 0 && nb > 0 && x < y + static_cast<uintptr_t>(nb) && y < x + static_cast<uintptr_t>(na);
+}
+
+// (T / rows + n_seq + 1) heads workgroups: fewer than a launch may have
+bool groups_ok(int64_t T, int rows, int64_t n_seq, int64_t heads) {
+  return heads == 0 || T / rows + n_seq + 1 <= (kMaxGroups - 1) / heads;
 }
 
 bool cache_sizes_ok(int64_t r, int64_t d_rope) {
@@ -100,8 +106,8 @@ lb_status lb_rotate(const void* x, lb_dtype dtype, int64_t T, int64_t H, int64_t
                     const int32_t* positions, const float* freqs, int inverse, void* y, int64_t y_t, int64_t y_h,
                     hipStream_t stream) {
   if (!dtype_ok(dtype)) return LB_ERR_DTYPE;
-  if (T < 0 || H < 0 || d < 0 || d % 2 != 0 || d > lb::kMaxRope || !fits(T, H, d) || !strides_ok(x_t, x_h) ||
-      !strides_ok(y_t, y_h))
+  if (T < 0 || H < 0 || d < 0 || d % 2 != 0 || d > lb::kMaxRope || !fits(T, H, d) || !strides_ok(T, H, x_t, x_h) ||
+      !strides_ok(T, H, y_t, y_h))
     return LB_ERR_SHAPE;
   if (T == 0 || H == 0 || d == 0) return LB_OK;
   if (!x || !y || !positions || !freqs) return LB_ERR_NULL;
@@ -125,7 +131,7 @@ lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const vo
   if (!dtype_ok(dtype)) return LB_ERR_DTYPE;
   lb_status st = check_cache(cache);
   if (st != LB_OK) return st;
-  if (T < 0 || !fits(T, lb::latent_row(cache->r, cache->d_rope)) || !strides_ok(k_rope_t, 0)) return LB_ERR_SHAPE;
+  if (T < 0 || !fits(T, lb::latent_row(cache->r, cache->d_rope)) || !stride_ok(T, k_rope_t)) return LB_ERR_SHAPE;
   if (T == 0 || cache->n_seq == 0) return LB_OK;
   if (!w || (cache->d_rope > 0 && !k_rope)) return LB_ERR_NULL;
   st = check_cache_ptrs(cache);
@@ -163,7 +169,7 @@ lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int6
   lb_status st = check_cache(cache);
   if (st != LB_OK) return st;
   if (T < 0 || H < 0 || Hk < 1 || H % Hk != 0 || d_nope < 0 || d_nope > 256 || d_v < 0 || d_v > 256 ||
-      !strides_ok(q_t, q_h) || !fits(T, H, lb::latent_row(cache->r, cache->d_rope)) ||
+      !strides_ok(T, H, q_t, q_h) || !fits(T, H, lb::latent_row(cache->r, cache->d_rope)) ||
       !fits(T, H, d_nope + cache->d_rope) || !fits(T, H, d_v) || !fits(Hk, d_nope + d_v, cache->r) || T * H >= kMaxRows)
     return LB_ERR_SHAPE;
   // the kernels count steps of 16 tokens or more of items of 32 query rows in 31 bits
@@ -213,13 +219,12 @@ lb_status check_attention(const lb_attention* a) {
   if (!dtype_ok(a->dtype)) return LB_ERR_DTYPE;
   if (a->Tq < 0 || a->Tk < 0 || a->H < 0 || a->Hk < 1 || a->H % a->Hk != 0 || a->d_nope < 0 || a->d_rope < 0 ||
       a->d_nope > 192 || a->d_rope > 192 || !lb::attn_supports(a->d_nope + a->d_rope, a->d_v) || a->n_seq < 0 ||
-      a->n_seq > (1 << 24) || !strides_ok(a->q_t, a->q_h) || !strides_ok(a->k_t, a->k_h) ||
-      !strides_ok(a->v_t, a->v_h) || !strides_ok(a->kr_t, 0))
+      a->n_seq > (1 << 24) || !strides_ok(a->Tq, a->H, a->q_t, a->q_h) || !strides_ok(a->Tk, a->Hk, a->k_t, a->k_h) ||
+      !strides_ok(a->Tk, a->Hk, a->v_t, a->v_h) || !stride_ok(a->Tk, a->kr_t))
     return LB_ERR_SHAPE;
   const int64_t dk = a->d_nope + a->d_rope;
   if (!fits(a->Tq, a->H, dk) || !fits(a->Tq, a->H, a->d_v) || !fits(a->Tk, a->Hk, dk) || !fits(a->Tk, a->Hk, a->d_v) ||
-      !fits(a->n_seq + 1, a->H) || (a->Tq / 128 + a->n_seq + 1) * a->H >= kMaxGroups ||
-      (a->Tk / 128 + a->n_seq + 1) * a->Hk >= kMaxGroups)
+      !fits(a->n_seq + 1, a->H) || !groups_ok(a->Tq, 128, a->n_seq, a->H) || !groups_ok(a->Tk, 128, a->n_seq, a->Hk))
     return LB_ERR_SHAPE;
   if ((a->cu_q == nullptr) != (a->cu_k == nullptr) || !scale_ok(a->scale)) return LB_ERR_ARG;
   return LB_OK;
@@ -290,7 +295,8 @@ lb_status lb_attention_backward(const lb_attention* a, const void* o, const floa
   lb_status st = check_attention(a);
   if (st != LB_OK) return st;
   if (!grads) return LB_ERR_NULL;
-  if (!strides_ok(grads->dk_t, grads->dk_h) || !strides_ok(grads->dv_t, grads->dv_h)) return LB_ERR_SHAPE;
+  if (!strides_ok(a->Tk, a->Hk, grads->dk_t, grads->dk_h) || !strides_ok(a->Tk, a->Hk, grads->dv_t, grads->dv_h))
+    return LB_ERR_SHAPE;
   if (a->H == 0 || (a->Tq == 0 && a->Tk == 0) || (a->cu_q && a->n_seq == 0)) return LB_OK;
   st = check_attention_ptrs(a);
   if (st != LB_OK) return st;

@@ -1,0 +1,144 @@
+// Host-side driver for the sanitizer build of the attention calls' boundary (csrc/attention_api.cpp).  The
+// launches are stand-ins that note what reaches them, so calls that are accepted can be checked too: no GPU is
+// used and no address is read.  Exits non-zero on the first unexpected result.
+#include <cstdint>
+#include <cstdio>
+#include <cstring>
+#include <initializer_list>
+
+#include "../../paper_2506_13771_amd/csrc/attn.h"
+
+static int launches = 0;
+static bool vec_fits = true;
+namespace lb {
+hipError_t launch_rotate(const RotateArgs&, hipStream_t) { return ++launches, hipSuccess; }
+hipError_t launch_append(const AppendArgs&, hipStream_t) { return ++launches, hipSuccess; }
+hipError_t launch_latent_attn(const LatentAttnArgs&, hipStream_t) { return ++launches, hipSuccess; }
+hipError_t launch_attn_forward(const AttnArgs&, hipStream_t) { return ++launches, hipSuccess; }
+hipError_t launch_attn_backward(const AttnArgs&, hipStream_t) { return ++launches, hipSuccess; }
+size_t latent_attn_workspace_bytes(int T, int n_seq, int H, int r, int d_rope) {
+  return 256 + 6 * static_cast<size_t>(T) * H * latent_row(r, d_rope) + n_seq;
+}
+bool attn_vec(const AttnArgs&, bool) { return vec_fits; }
+bool attn_supports(int64_t dk, int64_t dv) { return dk >= 1 && dk <= 192 && dv >= 1 && dv <= 128; }
+}  // namespace lb
+
+static int failures = 0;
+#define EXPECT(c)                                                              \
+  do {                                                                         \
+    if (!(c)) {                                                                \
+      std::fprintf(stderr, "%s:%d: failed: %s\n", __FILE__, __LINE__, #c);     \
+      ++failures;                                                              \
+    }                                                                          \
+  } while (0)
+// the status, and whether anything was launched: only ever an accepted call
+#define STATUS(call, want)                                                                        \
+  do {                                                                                            \
+    const int before = launches;                                                                  \
+    const lb_status got = (call);                                                                 \
+    if (got != (want)) std::fprintf(stderr, "%s:%d: status %d, not %d\n", __FILE__, __LINE__, got, want); \
+    EXPECT(got == (want));                                                                        \
+    EXPECT(got == LB_OK || launches == before);                                                   \
+  } while (0)
+
+// stand-ins for device addresses
+static void* at(int64_t i) { return reinterpret_cast<void*>(i << 34); }
+static constexpr int64_t kFar = int64_t(1) << 40, kMost = (int64_t(1) << 31) - 1;
+
+static lb_latent_cache cache() {
+  return lb_latent_cache{at(1), LB_BF16, 4, 16, 16, 8, static_cast<int32_t*>(at(2)), 2, 2, static_cast<int32_t*>(at(3)), static_cast<int32_t*>(at(4))};
+}
+static lb_attention attn() {
+  lb_attention a{};
+  a.q = at(10), a.k = at(12), a.v = at(14), a.k_rope = at(16);
+  a.dtype = LB_BF16;
+  a.Tq = 8, a.Tk = 9, a.H = 4, a.Hk = 2, a.d_nope = 32, a.d_rope = 16, a.d_v = 24;
+  a.q_t = 192, a.q_h = 48, a.k_t = 64, a.k_h = 32, a.v_t = 48, a.v_h = 24, a.kr_t = 16;
+  a.causal = 1, a.scale = 0.2f;
+  return a;
+}
+static lb_attention_grads grads() {
+  lb_attention_grads g{};
+  g.dq = at(20), g.dk = at(22), g.dv = at(24), g.dk_rope = at(26);
+  g.dk_t = 64, g.dk_h = 32, g.dv_t = 48, g.dv_h = 24;
+  return g;
+}
+static lb_status forward(const lb_attention& a, void* o = at(30), void* lse = at(32)) {
+  return lb_attention_forward(&a, o, static_cast<float*>(lse), nullptr);
+}
+static lb_status backward(const lb_attention& a, const lb_attention_grads& g, void* ws = at(40), size_t n = size_t(1) << 31) {
+  return lb_attention_backward(&a, at(30), static_cast<const float*>(at(32)), at(34), &g, ws, n, nullptr);
+}
+static lb_status latent(const lb_latent_cache& c, int64_t T = 3, int64_t H = 4, int64_t Hk = 2, int64_t q_t = 160, int64_t q_h = 40,
+                        void* out = at(50), void* ws = at(60), int64_t dn = 32, int64_t dv = 16) {
+  static lb_path p[2];
+  for (auto& x : p) x = lb_path{at(70), nullptr, at(72), nullptr, nullptr};
+  return lb_latent_attention(at(74), LB_BF16, T, H, Hk, dn, dv, q_t, q_h, p, LB_F16, &c, static_cast<float*>(at(76)), 0.1f, out, ws,
+                             size_t(1) << 40, nullptr);
+}
+static lb_status rotate(int64_t T, int64_t H, int64_t d, int64_t x_t, int64_t x_h, int64_t y_t, int64_t y_h) {
+  return lb_rotate(at(80), LB_F32, T, H, d, x_t, x_h, static_cast<int32_t*>(at(2)), static_cast<float*>(at(3)), 0, at(4),
+                   y_t, y_h, nullptr);
+}
+
+// Sizes and strides whose products pass 64 bits
+static void offsets() {
+  EXPECT(forward(attn()) == LB_OK && backward(attn(), grads()) == LB_OK && latent(cache()) == LB_OK && launches == 3);
+  STATUS(rotate(2, 3, 8, 24, 8, 24, 8), LB_OK);
+  // (an operand's last element may lie 2^59 elements behind its first)
+  STATUS(rotate(1 << 19, 1, 8, kFar, 0, 8, 8), LB_OK);
+  STATUS(rotate(1 << 28, 1, 2, kFar, 0, 8, 8), LB_ERR_SHAPE);
+  STATUS(rotate(1, 1 << 28, 2, 8, kFar, 8, 8), LB_ERR_SHAPE);
+  STATUS(rotate(1 << 28, 1, 2, 8, 8, kFar, 8), LB_ERR_SHAPE);
+  STATUS(rotate(1, 1 << 28, 2, 8, 8, 8, kFar), LB_ERR_SHAPE);
+  STATUS(rotate(1, 1, 2, kFar, kFar, kFar, kFar), LB_OK);
+  for (int64_t T : {kMost / 32, int64_t(1) << 25}) {
+    lb_attention a = attn();
+    a.H = a.Hk = 1, a.d_nope = 8, a.d_rope = 0, a.d_v = 8, a.Tq = a.Tk = T;
+    a.q_t = a.k_t = a.v_t = 8;
+    lb_attention_grads g = grads();
+    g.dk_t = g.dv_t = 8;
+    STATUS(forward(a), LB_OK);
+    STATUS(backward(a, g), LB_OK);
+    for (int64_t lb_attention::*s : {&lb_attention::q_t, &lb_attention::k_t, &lb_attention::v_t}) {
+      lb_attention b = a;
+      b.*s = kFar;
+      STATUS(forward(b), LB_ERR_SHAPE);
+      STATUS(backward(b, g), LB_ERR_SHAPE);
+    }
+    lb_attention b = a;
+    b.d_rope = 8, b.kr_t = kFar;
+    STATUS(forward(b), LB_ERR_SHAPE);
+    for (int64_t lb_attention_grads::*s : {&lb_attention_grads::dk_t, &lb_attention_grads::dv_t}) {
+      lb_attention_grads h = g;
+      h.*s = kFar;
+      STATUS(backward(a, h), LB_ERR_SHAPE);
+    }
+    lb_latent_cache c = cache();
+    STATUS(lb_latent_append(&c, at(90), at(1 << 20), kFar, LB_F32, T, nullptr, nullptr), LB_ERR_SHAPE);
+  }
+  lb_latent_cache c = cache();
+  STATUS(latent(c, 1 << 20, 1, 1, kFar, 40), LB_ERR_SHAPE);
+  STATUS(latent(c, 1, 1 << 20, 1, 40, kFar), LB_ERR_SHAPE);
+  // no queries' heads: any number of key heads divides them
+  for (int64_t n : {int64_t(3), int64_t(1) << 24}) {
+    lb_attention a = attn();
+    a.H = 0, a.Hk = int64_t(1) << 62, a.Tk = 0, a.n_seq = n;
+    a.cu_q = a.cu_k = static_cast<int32_t*>(at(5));
+    STATUS(forward(a), LB_ERR_SHAPE);
+    STATUS(backward(a, grads()), LB_ERR_SHAPE);
+  }
+  for (int64_t n : {int64_t(0), int64_t(1), int64_t(33), kMost, int64_t(1) << 40, INT64_MAX}) {
+    for (int64_t m : {int64_t(0), int64_t(1), kMost, INT64_MAX}) {
+      (void)lb_latent_row(n, m), (void)lb_latent_attention_workspace_bytes(n, m, 1, 16, 8);
+      (void)lb_latent_attention_workspace_bytes(n, 1, m, 16, 8), (void)lb_attention_backward_workspace_bytes(n, m, 1, 1, 64);
+      (void)lb_attention_backward_workspace_bytes(n, 1, m, 1, 0), (void)lb_attention_backward_workspace_bytes(1, n, 0, m > 0 ? m : 1, 64);
+    }
+  }
+}
+
+int main() {
+  offsets();
+  if (failures == 0) std::printf("sanitized attention checks passed\n");
+  return failures == 0 ? 0 : 1;
+}
