@@ -526,7 +526,7 @@ lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const vo
    query's position (freqs; NULL: taken as they are); out [T x H x d_v]
    contiguous, in act_dtype.  A query that sees no token gets 0.  Only U and h of
    the paths are read (of the fused layer, d_out = Hk (d_nope + d_v)).  H a
-   multiple of Hk; d_nope, d_v <= 256; T H < 2^22; (T H / 32 + n_seq) (max_pages page_size / 16
+   multiple of Hk; d_nope, d_v <= 256; T H < 2^22; 2 ceil(r / 32) ceil(T / 32) H + T ceil(H / 8) < 2^26; (T H / 32 + n_seq) (max_pages page_size / 16
    + 1) < 2^31 (LB_ERR_SHAPE); scale finite and > 0
    (LB_ERR_ARG).  q' enters the scores with at least 16 significant bits (24 for
    fp32 activations; over an f16 cache 22 of values down to 2^-17, and 16 down to 2^-22, of the larger of
@@ -554,7 +554,8 @@ lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int6
    both NULL for one sequence of all rows.  causal != 0: query i of n_q sees keys
    j <= i + n_k - n_q of its sequence.  Query head h reads key head h / (H / Hk).
    1 <= d_nope + d_rope <= 192, 1 <= d_v <= 128, (Tq / 128 + n_seq + 1) H and (Tk /
-   128 + n_seq + 1) Hk < 2^24 (LB_ERR_SHAPE); scale finite and > 0 (LB_ERR_ARG).
+   128 + n_seq + 1) Hk < 2^24, with 32 for 128 where 16-bit operands are not all aligned to 16 bytes
+   and of widths and strides that are multiples of 8 (LB_ERR_SHAPE); scale finite and > 0 (LB_ERR_ARG).
    Rows behind cu_q[n_seq] / cu_k[n_seq] are neither read nor
    written; accesses stay inside the buffers whatever cu_q and cu_k hold.  A
    masked score is left out whatever its key holds, but a NaN or infinity in v may

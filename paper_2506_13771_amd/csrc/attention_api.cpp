@@ -24,8 +24,8 @@ int64_t dtype_size(lb_dtype d) { return d == LB_F32 ? 4 : 2; }
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 // a launch's threads are counted in 32 bits: rows (token, head) with a workgroup of up to
-// 1024 threads each, and workgroups of 256
-constexpr int64_t kMaxRows = int64_t(1) << 22, kMaxGroups = int64_t(1) << 24;
+// 1024 threads each, workgroups of 256, and single waves
+constexpr int64_t kMaxRows = int64_t(1) << 22, kMaxGroups = int64_t(1) << 24, kMaxWaves = int64_t(1) << 26;
 
 // a b (and a b c) below 2^31, all factors >= 0
 bool fits(int64_t a, int64_t b) { return a == 0 || b <= kMaxElems / a; }
@@ -172,6 +172,9 @@ lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int6
       !strides_ok(T, H, q_t, q_h) || !fits(T, H, lb::latent_row(cache->r, cache->d_rope)) ||
       !fits(T, H, d_nope + cache->d_rope) || !fits(T, H, d_v) || !fits(Hk, d_nope + d_v, cache->r) || T * H >= kMaxRows)
     return LB_ERR_SHAPE;
+  // single waves of absorb: 32 latents, 32 tokens and a head, or eight heads' rotary part
+  const int64_t waves = 2 * ((cache->r + 31) / 32) * ((T + 31) / 32) * H + T * ((H + 7) / 8);
+  if (waves >= kMaxWaves) return LB_ERR_SHAPE;
   // the kernels count steps of 16 tokens or more of items of 32 query rows in 31 bits
   if (!fits(T * H / 32 + cache->n_seq, cache->max_pages * cache->page_size / 16 + 1)) return LB_ERR_SHAPE;
   if (!scale_ok(scale)) return LB_ERR_ARG;
@@ -238,6 +241,12 @@ lb_status check_attention_ptrs(const lb_attention* a) {
     return LB_ERR_ALIGN;
   return LB_OK;
 }
+// 16-bit operands that cannot be read 16 bytes at a time have 32 rows a workgroup (otherwise 32
+// only where that makes few)
+bool launch_ok(const lb::AttnArgs& a, bool backward) {
+  const int rows = a.dt != LB_F32 && !lb::attn_vec(a, backward) ? 32 : 128;
+  return groups_ok(a.Tq, rows, a.n_seq, a.H) && (!backward || groups_ok(a.Tk, rows, a.n_seq, a.Hk));
+}
 lb::AttnArgs attention_args(const lb_attention* a) {
   lb::AttnArgs r{};
   r.q = a->q, r.k = a->k, r.v = a->v, r.k_rope = a->k_rope;
@@ -278,6 +287,7 @@ lb_status lb_attention_forward(const lb_attention* a, void* o, float* lse, hipSt
     return LB_ERR_ARG;
   lb::AttnArgs r = attention_args(a);
   r.o = o, r.lse = lse;
+  if (!launch_ok(r, false)) return LB_ERR_SHAPE;
   return hip_status(lb::launch_attn_forward(r, stream));
 }
 
@@ -320,6 +330,7 @@ lb_status lb_attention_backward(const lb_attention* a, const void* o, const floa
   r.d_o = d_o;
   r.dq = grads->dq, r.dk = grads->dk, r.dv = grads->dv, r.dkr = grads->dk_rope;
   r.dk_t = grads->dk_t, r.dk_h = grads->dk_h, r.dv_t = grads->dv_t, r.dv_h = grads->dv_h;
+  if (!launch_ok(r, true)) return LB_ERR_SHAPE;
   char* ws = static_cast<char*>(workspace);
   r.delta = reinterpret_cast<float*>(ws);
   r.dkr_part = reinterpret_cast<float*>(ws + up256(a->Tq * a->H * 4));

@@ -137,8 +137,45 @@ static void offsets() {
   }
 }
 
+// Calls whose launch would have 2^32 threads
+static void launch_sizes() {
+  for (const bool vec : {true, false}) {
+    vec_fits = vec;
+    for (const lb_dtype dt : {LB_F32, LB_F16, LB_BF16}) {
+      const int64_t rows = dt == LB_F32 || vec ? 128 : 32;
+      for (const int64_t H : {int64_t(1), int64_t(64), int64_t(4096)}) {
+        lb_attention a = attn();
+        a.dtype = dt, a.H = a.Hk = H, a.d_nope = 2, a.d_rope = 0, a.d_v = 2;
+        a.q_t = a.k_t = a.v_t = 2 * H, a.q_h = a.k_h = a.v_h = 2;
+        lb_attention_grads g = grads();
+        g.dk_t = g.dv_t = 2 * H, g.dk_h = g.dv_h = 2;
+        const int64_t most = ((int64_t(1) << 24) - 1) / H;  // T / rows + 1
+        if ((most * rows) * H * 2 <= kMost) {
+          a.Tq = a.Tk = (most - 1) * rows + rows - 1;
+          STATUS(forward(a), LB_OK);
+          STATUS(backward(a, g), LB_OK);
+        }
+        if ((most * rows + rows) * H * 2 > kMost) continue;
+        a.Tq = most * rows, a.Tk = 1;
+        STATUS(forward(a), LB_ERR_SHAPE);
+        STATUS(backward(a, g), LB_ERR_SHAPE);
+        a.Tq = 1, a.Tk = most * rows;
+        STATUS(forward(a), LB_OK);
+        STATUS(backward(a, g), LB_ERR_SHAPE);
+      }
+    }
+  }
+  vec_fits = true;
+  lb_latent_cache c = cache();
+  c.r = 704, c.d_rope = 0;
+  // 44 waves a head, and one for eight heads
+  STATUS(latent(c, 1, 1500000, 1, 40, 0, at(50), at(60), 1, 1), LB_OK);
+  STATUS(latent(c, 1, 1524000, 1, 40, 0, at(50), at(60), 1, 1), LB_ERR_SHAPE);
+}
+
 int main() {
   offsets();
+  launch_sizes();
   if (failures == 0) std::printf("sanitized attention checks passed\n");
   return failures == 0 ? 0 : 1;
 }
