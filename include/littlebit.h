@@ -537,7 +537,8 @@ lb_status lb_latent_append(const lb_latent_cache* cache, const void* w, const vo
    which do not see it (a zero probability is multiplied with it).
    workspace: 256-byte aligned, >= lb_latent_attention_workspace_bytes(T, n_seq,
    H, r, d_rope) bytes (0 for invalid sizes), no zero-fill needed; calls that may
-   run concurrently need distinct workspaces.  Repeated calls give the same bits. */
+   run concurrently need distinct workspaces.  out may not overlap q or the cache, nor
+   the workspace any of the three (LB_ERR_ARG).  Repeated calls give the same bits. */
 size_t lb_latent_attention_workspace_bytes(int64_t T, int64_t n_seq, int64_t H, int64_t r, int64_t d_rope);
 lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int64_t H, int64_t Hk, int64_t d_nope,
                               int64_t d_v, int64_t q_t, int64_t q_h, const lb_path* paths, lb_dtype scale_dtype,
@@ -585,7 +586,8 @@ lb_status lb_attention_forward(const lb_attention* a, void* o, float* lse, hipSt
    P and dS are rounded to dtype for their products (dS for dq of heads up to 128
    wide to two terms of it).  Gradients of grouped heads
    are summed in a fixed order: repeated calls give the same bits.  No output may
-   overlap an input or another output (not checked).  If H is 0 nothing is written.  workspace: 256-byte
+   overlap an input, another output or the workspace (LB_ERR_ARG; parts of one buffer that
+   interleave by their strides are apart).  If H is 0 nothing is written.  workspace: 256-byte
    aligned, >= lb_attention_backward_workspace_bytes(Tq, Tk, H, Hk, d_rope)
    bytes (0 for invalid sizes), no zero-fill needed. */
 typedef struct lb_attention_grads {

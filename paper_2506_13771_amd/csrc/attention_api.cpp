@@ -2,6 +2,7 @@
 // and launch.  Nothing is enqueued unless every check has passed.
 #include <cmath>
 #include <cstring>
+#include <numeric>
 
 #include "attn.h"
 
@@ -47,6 +48,34 @@ bool rows_apart(int64_t T, int64_t H, int64_t d, int64_t st, int64_t sh) {
 bool ranges_meet(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return na > 0 && nb > 0 && x < y + static_cast<uintptr_t>(nb) && y < x + static_cast<uintptr_t>(na);
+}
+
+// Bytes of an operand: T x H rows of d at strides st, sh; or n bytes in a row.
+struct Region {
+  uintptr_t p;
+  int64_t T, H, d, st, sh;
+};
+Region rows_of(const void* p, int64_t T, int64_t H, int64_t d, int64_t st, int64_t sh, int64_t es) {
+  return Region{reinterpret_cast<uintptr_t>(p), T, H, d * es, T > 1 ? st * es : 0, H > 1 ? sh * es : 0};
+}
+Region bytes_of(const void* p, int64_t n) { return Region{reinterpret_cast<uintptr_t>(p), 1, 1, n, 0, 0}; }
+// [p, p + e) and [q, q + f), both repeated every g bytes, apart?
+bool repeats_apart(uintptr_t p, int64_t e, uintptr_t q, int64_t f, int64_t g) {
+  if (g == 0 || e > g || f > g) return false;
+  const int64_t m = q >= p ? static_cast<int64_t>((q - p) % g) : (g - static_cast<int64_t>((p - q) % g)) % g;
+  return m >= e && m + f <= g;
+}
+// Whether two operands may share a byte.  Where their spans meet, parts of one buffer are still apart if
+// their rows, whole tokens or whole heads keep to places of their own within a common period of the strides.
+bool operands_meet(const Region& a, const Region& b) {
+  if (a.T <= 0 || a.H <= 0 || a.d <= 0 || b.T <= 0 || b.H <= 0 || b.d <= 0) return false;
+  const int64_t ea = (a.H - 1) * a.sh + a.d, eb = (b.H - 1) * b.sh + b.d;  // a token's bytes, all heads
+  const int64_t fa = (a.T - 1) * a.st + a.d, fb = (b.T - 1) * b.st + b.d;  // a head's, all tokens
+  const uintptr_t na = static_cast<uintptr_t>((a.T - 1) * a.st + ea), nb = static_cast<uintptr_t>((b.T - 1) * b.st + eb);
+  if (a.p >= b.p + nb || b.p >= a.p + na) return false;
+  const int64_t gt = std::gcd(a.st, b.st), gh = std::gcd(a.sh, b.sh);
+  return !repeats_apart(a.p, a.d, b.p, b.d, std::gcd(gt, gh)) && !repeats_apart(a.p, ea, b.p, eb, gt) &&
+         !repeats_apart(a.p, fa, b.p, fb, gh);
 }
 
 // (T / rows + n_seq + 1) heads workgroups: fewer than a launch may have
@@ -197,6 +226,10 @@ lb_status lb_latent_attention(const void* q, lb_dtype act_dtype, int64_t T, int6
   if (!workspace) return LB_ERR_NULL;
   if (!aligned(workspace, 256)) return LB_ERR_ALIGN;
   if (workspace_bytes < need) return LB_ERR_WORKSPACE;
+  const Region ws = bytes_of(workspace, static_cast<int64_t>(need));
+  if (operands_meet(ws, bytes_of(out, no)) || operands_meet(ws, bytes_of(cache->data, nc)) ||
+      operands_meet(ws, rows_of(q, T, H, d_nope + cache->d_rope, q_t, q_h, es)))
+    return LB_ERR_ARG;
   lb::LatentAttnArgs a{};
   a.c = cache_args(cache);
   a.q = q;
@@ -331,6 +364,21 @@ lb_status lb_attention_backward(const lb_attention* a, const void* o, const floa
   r.dq = grads->dq, r.dk = grads->dk, r.dv = grads->dv, r.dkr = grads->dk_rope;
   r.dk_t = grads->dk_t, r.dk_h = grads->dk_h, r.dv_t = grads->dv_t, r.dv_h = grads->dv_h;
   if (!launch_ok(r, true)) return LB_ERR_SHAPE;
+  const int64_t dk = a->d_nope + a->d_rope, no = a->Tq * a->H * a->d_v * es;
+  const Region in[] = {rows_of(a->q, a->Tq, a->H, dk, a->q_t, a->q_h, es), rows_of(a->k, a->Tk, a->Hk, a->d_nope, a->k_t, a->k_h, es),
+                       rows_of(a->v, a->Tk, a->Hk, a->d_v, a->v_t, a->v_h, es), rows_of(a->k_rope, a->Tk, 1, a->d_rope, a->kr_t, 0, es),
+                       bytes_of(o, no), bytes_of(lse, a->Tq * a->H * 4), bytes_of(d_o, no)};
+  const Region out[] = {bytes_of(grads->dq, a->Tq * a->H * dk * es),
+                        rows_of(grads->dk, a->Tk, a->Hk, a->d_nope, grads->dk_t, grads->dk_h, es),
+                        rows_of(grads->dv, a->Tk, a->Hk, a->d_v, grads->dv_t, grads->dv_h, es),
+                        bytes_of(grads->dk_rope, a->Tk * a->d_rope * es), bytes_of(workspace, static_cast<int64_t>(need))};
+  constexpr int n_out = sizeof out / sizeof *out;
+  for (int i = 0; i < n_out; ++i) {
+    for (const Region& x : in)
+      if (operands_meet(out[i], x)) return LB_ERR_ARG;
+    for (int j = i + 1; j < n_out; ++j)
+      if (operands_meet(out[i], out[j])) return LB_ERR_ARG;
+  }
   char* ws = static_cast<char*>(workspace);
   r.delta = reinterpret_cast<float*>(ws);
   r.dkr_part = reinterpret_cast<float*>(ws + up256(a->Tq * a->H * 4));

@@ -173,8 +173,81 @@ static void launch_sizes() {
   STATUS(latent(c, 1, 1524000, 1, 40, 0, at(50), at(60), 1, 1), LB_ERR_SHAPE);
 }
 
+// Operands that share bytes, and parts of one buffer that do not
+static void overlaps() {
+  const int64_t T = 9, H = 4, Hk = 2, dn = 32, dr = 16, dv = 24, es = 2;
+  lb_attention a = attn();
+  const lb_attention_grads far = grads();
+  STATUS(backward(a, far), LB_OK);
+  auto plus = [](const void* p, int64_t n) { return const_cast<char*>(static_cast<const char*>(p)) + n; };
+  const void* in[] = {a.q, a.k, a.v, a.k_rope, at(30), at(32), at(34)};
+  const int64_t in_bytes[] = {((a.Tq - 1) * a.q_t + (H - 1) * a.q_h + dn + dr) * es, ((T - 1) * a.k_t + (Hk - 1) * a.k_h + dn) * es,
+                              ((T - 1) * a.v_t + (Hk - 1) * a.v_h + dv) * es, ((T - 1) * a.kr_t + dr) * es, a.Tq * H * dv * es,
+                              a.Tq * H * 4, a.Tq * H * dv * es};
+  const int64_t out_bytes[] = {a.Tq * H * (dn + dr) * es, ((T - 1) * far.dk_t + (Hk - 1) * far.dk_h + dn) * es,
+                               ((T - 1) * far.dv_t + (Hk - 1) * far.dv_h + dv) * es, T * dr * es};
+  auto put = [&](int o, void* p) {
+    lb_attention_grads g = far;
+    (o == 0 ? g.dq : o == 1 ? g.dk : o == 2 ? g.dv : g.dk_rope) = p;
+    return backward(a, g);
+  };
+  for (int o = 0; o < 4; ++o) {
+    for (int i = 0; i < 7; ++i) {
+      STATUS(put(o, plus(in[i], 0)), LB_ERR_ARG);
+      STATUS(put(o, plus(in[i], in_bytes[i] - 2)), LB_ERR_ARG);
+      STATUS(put(o, plus(in[i], in_bytes[i])), LB_OK);
+      STATUS(put(o, plus(in[i], 2 - out_bytes[o])), LB_ERR_ARG);
+      STATUS(put(o, plus(in[i], -out_bytes[o])), LB_OK);
+    }
+    const void* out[] = {far.dq, far.dk, far.dv, far.dk_rope};
+    for (int p = 0; p < 4; ++p) {
+      if (p == o) continue;
+      STATUS(put(o, plus(out[p], 0)), LB_ERR_ARG);
+      STATUS(put(o, plus(out[p], out_bytes[p])), LB_OK);
+    }
+    STATUS(backward(a, far, plus(out[o], 0)), LB_ERR_ARG);
+  }
+  for (int i = 0; i < 7; ++i) STATUS(backward(a, far, plus(in[i], 0)), LB_ERR_ARG);
+  // the two parts of the fused layer's dy, and heads that hold key and value next to each other
+  lb_attention_grads g = far;
+  g.dk_t = g.dv_t = Hk * (dn + dv), g.dv = plus(g.dk, Hk * dn * es);
+  STATUS(backward(a, g), LB_OK);
+  g.dv = plus(g.dk, (Hk * dn - 1) * es);
+  STATUS(backward(a, g), LB_ERR_ARG);
+  g.dv = plus(g.dk, (Hk * dn + 1) * es);  // the last value's end is the next token's first key
+  STATUS(backward(a, g), LB_ERR_ARG);
+  g.dk_h = g.dv_h = dn + dv, g.dv = plus(g.dk, dn * es);
+  STATUS(backward(a, g), LB_OK);
+  g.dv = plus(g.dk, dn * es - 2);
+  STATUS(backward(a, g), LB_ERR_ARG);
+  // tokens inside heads
+  g.dk_t = dn, g.dv_t = dv, g.dk_h = g.dv_h = T * (dn + dv), g.dv = plus(g.dk, T * dn * es);
+  STATUS(backward(a, g), LB_OK);
+  g.dv = plus(g.dv, -2);
+  STATUS(backward(a, g), LB_ERR_ARG);
+  // gradients in the spare columns of the operands' own buffer
+  lb_attention b = a;
+  b.k_t = 2 * Hk * dn, g = far;
+  g.dk = plus(b.k, Hk * dn * es), g.dk_t = b.k_t;
+  STATUS(backward(b, g), LB_OK);
+  g.dk = plus(g.dk, -2);
+  STATUS(backward(b, g), LB_ERR_ARG);
+  // one token: strides do not count
+  b.Tk = 1, b.k_t = 0, g = far, g.dk = plus(b.k, (Hk * dn) * es), g.dk_t = 0;
+  STATUS(backward(b, g), LB_OK);
+  // the latent attention's workspace
+  const lb_latent_cache c = cache();
+  STATUS(latent(c, 3, 4, 2, 160, 40, at(50), at(74)), LB_ERR_ARG);
+  STATUS(latent(c, 3, 4, 2, 160, 40, at(50), at(1)), LB_ERR_ARG);
+  STATUS(latent(c, 3, 4, 2, 160, 40, at(50), at(50)), LB_ERR_ARG);
+  const int64_t need = static_cast<int64_t>(lb_latent_attention_workspace_bytes(3, 2, 4, 16, 8));
+  STATUS(latent(c, 3, 4, 2, 160, 40, plus(at(60), need - 2), at(60)), LB_ERR_ARG);
+  STATUS(latent(c, 3, 4, 2, 160, 40, plus(at(60), need + need % 2), at(60)), LB_OK);
+}
+
 int main() {
   offsets();
+  overlaps();
   launch_sizes();
   if (failures == 0) std::printf("sanitized attention checks passed\n");
   return failures == 0 ? 0 : 1;
