@@ -601,6 +601,10 @@ def _whole(t, shape, dtype, name: str) -> int:
     return t.data_ptr()
 
 
+def _default_scale(width: int) -> float:
+    return max(width, 1) ** -0.5
+
+
 def _freqs(t, d: int) -> int:
     return 0 if t is None else _whole(t, (d // 2,), _T.float32, "freqs")
 
@@ -727,7 +731,7 @@ def lb_latent_attention(q, cache: LatentCache, paths: Sequence[LittleBitPath], H
     pq, sq = _rows(q, "q")
     st = load_library().lb_latent_attention(
         pq, _dtype_code(q), T, H, Hk, dn, d_v, sq[0], sq[1], arr, _dtype_code(a.h), cache._packed(table, lens, cu),
-        _freqs(freqs, dr), dq ** -0.5 if scale is None else scale, _whole(out, (T, H, d_v), q.dtype, "out"),
+        _freqs(freqs, dr), _default_scale(dq) if scale is None else scale, _whole(out, (T, H, d_v), q.dtype, "out"),
         _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream))
     if st:
         _check(st, "lb_latent_attention")
@@ -763,7 +767,7 @@ def _packed_attention(q, k, v, k_rope, cu_q, cu_k, causal, scale):
         pcq = _whole(cu_q, (n + 1,), _T.int32, "cu_q")
         pck = _whole(cu_k, (n + 1,), _T.int32, "cu_k")
     return _PACK_ATTN(pq, pk, pv, pr, _dtype_code(q), Tq, Tk, H, Hk, dn, dr, d_v, sq[0], sq[1], sk[0], sk[1], sv[0], sv[1],
-                      kr_t, pcq, pck, n, 1 if causal else 0, dq ** -0.5 if scale is None else scale), (
+                      kr_t, pcq, pck, n, 1 if causal else 0, _default_scale(dq) if scale is None else scale), (
                           Tq, Tk, H, Hk, dn, dr, d_v)
 
 

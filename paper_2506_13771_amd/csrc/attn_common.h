@@ -248,7 +248,10 @@ __device__ const uint32_t kZeros[4] = {0u, 0u, 0u, 0u};
 
 // 64 lanes' 16 bytes each from memory into LDS at dst (the same for all lanes) + 16 lane.
 // Written as assembly (it has no output register) so that the compiler does not wait for it
-// before the next read of any LDS; wait_loads() does.  (Nothing else here uses m0.)
+// before the next read of any LDS; wait_loads() does.  m0 is a reserved register, which a clobber
+// list cannot name: the compiler keeps nothing in it, and the instructions for which it would set
+// it (sends, global data share, indexed registers) do not occur here: in these kernels' assembly
+// every m0 is this block's.
 __device__ __forceinline__ void load_lds16(const void* src, char* dst) {
   const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)dst));
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
@@ -393,8 +396,9 @@ __device__ __forceinline__ bool find_tile(const int32_t* cu, int n_seq, int T, i
 // position rotation
 // ---------------------------------------------------------------------------
 // cos and sin of position * frequency.  The angle is formed and brought to one turn in
-// 64 bits (exact to 2^-21 of a turn's last fp32 place at positions up to 2^31), the
-// functions are taken in fp32 of the remaining half turn.
+// 64 bits: three roundings of 2^-53 of the number of turns, so off by 2^-44 of a turn near 160 turns (position 1000
+// at frequency 1), by 2^-23 at the 3.4e8 turns of position 2^31.  The functions are taken in fp32 of the
+// remaining half turn, whose rounding is up to 2^-26 of a turn.
 __device__ __forceinline__ void turn_of(int position, float freq, float& c, float& s) {
   const double t = static_cast<double>(position) * static_cast<double>(freq) * 0.15915494309189533577;
   const float f = static_cast<float>(t - rint(t));  // turns, in [-1/2, 1/2]

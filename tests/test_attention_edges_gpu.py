@@ -399,3 +399,25 @@ def test_a_nan_query_is_not_taken_for_one_that_sees_nothing(dtype, H):
     fine = torch.ones(70, H, dtype=torch.bool)
     fine[5, 0] = False
     assert bool(torch.isfinite(o.cpu()[fine]).all()) and bool(torch.isfinite(dq.cpu()[fine]).all())
+
+
+# ----------------------------------------------------------------------------
+# heads without a width
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("act", ["f32", "bf16", "f16"])
+def test_queries_of_width_0_average_the_values(act):
+    # no columns to score with: every cached token counts alike (scale left out)
+    lens, H, dv, r = [1, 50, 300], 3, 16, 20
+    g = _gen(81)
+    P = Paged(g, lens, [1, 1, 1], r, 0, 16, act)
+    paths, up = _layer(g, r, H * dv)
+    q = torch.zeros(3, H, 0, dtype=DT[act])
+    out = lb.lb_latent_attention(q.cuda(), P.cache, paths, H, dv, *P.meta)
+    ref, bound = R.latent_attention(q, P.rows, up, H, dv, lens, [1, 1, 1], None, 0, 1.0, DT[act])
+    _within(out, ref, bound, act)
+
+
+def test_expanded_queries_of_width_0_are_refused_by_the_library():
+    q, k, v = (torch.zeros(4, 2, d, device="cuda") for d in (0, 0, 8))
+    with pytest.raises(RuntimeError, match="lb_attention_forward"):
+        lb.lb_attention_forward(q, k, v)
