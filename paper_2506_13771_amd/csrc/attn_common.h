@@ -197,11 +197,11 @@ __device__ __forceinline__ void tile_put(char* tile, int t, int col, const Frag<
   if constexpr (DT == kDtF32) *reinterpret_cast<u32x4*>(p + 16 * ((q + 1) ^ s)) = f.v[1];
 }
 // A or B operand from rows: lane l takes row row0 + l % 32, columns col + 8 (l / 32) .. + 7
-// (row0 a multiple of 32, col of 16)
+// (row0 a multiple of 32, col of 16; a tile of 16 rows gives each twice: last_row 15)
 template <int DT, int R>
-__device__ __forceinline__ Frag<DT> frag_rows(const char* tile, int row0, int col, int lane) {
+__device__ __forceinline__ Frag<DT> frag_rows(const char* tile, int row0, int col, int lane, int last_row = 31) {
   constexpr int PU = pieces<DT>();
-  const int t = lane & 31, s = swz<DT>(t);
+  const int t = lane & last_row, s = swz<DT>(t);
   const char* p = tile + t * PU * 16;
   const int o = ((col >> 5) * R + row0) * PU * 16;
   Frag<DT> f;

@@ -452,57 +452,8 @@ struct SplitArgs {
   float* o;
 };
 
-// An LDS tile holds its tokens' columns of one wave, unit by unit: a unit's rows of PU
-// 16-byte pieces (4; fp32: 8), piece q of row t at q ^ unit_swz(t).  Row-wise reads (16
-// rows at one piece) then meet 16 different slots of the 64 banks, transposed reads
-// (8 rows of 4 pieces) each slot twice, the least.
-template <int CD>
-__device__ __forceinline__ int unit_swz(int t) {
-  return CD == kDtF32 ? (t >> 1) & 7 : (t >> 2) & 3;
-}
-// row lane % tpt of a unit at columns 16 half + 8 (lane / 32) ..
-template <int CD>
-__device__ __forceinline__ Frag<CD> tile_rows(const char* unit, int tpt, int half, int lane) {
-  constexpr int PU = 2 * esize<CD>();
-  const int t = lane & (tpt - 1), s = unit_swz<CD>(t);
-  const char* p = unit + t * PU * 16;
-  Frag<CD> f;
-  if constexpr (CD == kDtF32) {
-    const int q = 4 * half + 2 * (lane >> 5);
-    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * (q ^ s));
-    f.v[1] = *reinterpret_cast<const u32x4*>(p + 16 * ((q + 1) ^ s));
-  } else {
-    f.v[0] = *reinterpret_cast<const u32x4*>(p + 16 * ((2 * half + (lane >> 5)) ^ s));
-  }
-  return f;
-}
-// columns lane % 32 of a unit at the 16 tokens of slice s (slots as in attn_common.h)
-template <int CD>
-__device__ __forceinline__ Frag<CD> tile_cols(const char* t, int s, int lane) {
-  constexpr int PU = 2 * esize<CD>();
-  Frag<CD> f;
-  const int hh = lane >> 5;
-  if constexpr (CD == kDtF32) {
-    const int q = (lane & 31) >> 2;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int row = 16 * s + 8 * (k >> 2) + 4 * hh + (k & 3);
-      f.v[k >> 2][k & 3] =
-          *reinterpret_cast<const uint32_t*>(t + row * PU * 16 + 16 * (q ^ unit_swz<CD>(row)) + 4 * (lane & 3));
-    }
-  } else {
-    typedef __attribute__((address_space(3))) s16x4* lds4;
-    const int i = lane & 15, q = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-    const int row = 16 * s + 4 * hh + (i >> 2);
-    const char* p0 = t + row * PU * 16 + 16 * (q ^ unit_swz<CD>(row)) + 8 * (i & 1);
-    const char* p1 = t + (row + 8) * PU * 16 + 16 * (q ^ unit_swz<CD>(row + 8)) + 8 * (i & 1);
-    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0)));
-    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1)));
-    f.v[0] = u32x4{a[0], a[1], b[0], b[1]};
-  }
-  return f;
-}
-
+// An LDS tile holds its tokens' columns of one wave, unit by unit as in attn_common.h (whose
+// frag_rows and frag_cols read a unit as a tile of one): 32 rows, or 16.
 // a cache row of zeros (the widest, 4 bytes a column)
 __device__ const uint32_t kZeroRow[kMaxLatentRow] = {};
 
@@ -570,7 +521,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
       for (int n = 0; n < NL; ++n) {
         const int t = lane / PU + n * TPL;
         const int of = __shfl(idx, t & (p.tpt - 1));
-        src[n] = (of < 0 ? zeros : data + of * row_bytes) + 16 * ((lane & (PU - 1)) ^ unit_swz<CD>(t));
+        src[n] = (of < 0 ? zeros : data + of * row_bytes) + 16 * ((lane & (PU - 1)) ^ swz<CD>(t));
       }
 #pragma unroll
       for (int u = 0; u < UPW; ++u) {
@@ -672,7 +623,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
         const char* unit = tile + (EXACT ? u : min(u, nu - 1)) * unit_bytes;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const Frag<CD> kf = tile_rows<CD>(unit, p.tpt, k, lane);
+          const Frag<CD> kf = frag_rows<CD, 32>(unit, 0, 16 * k, lane, p.tpt - 1);
 #pragma unroll
           for (int n = 0; n < TQ; ++n) acc = mma32<CD>(kf, qf[2 * u + k][n], acc);
         }
@@ -742,7 +693,7 @@ __global__ void __launch_bounds__(256, 1) split_kernel(SplitArgs a) {
         // (the rotary units too: their sums are not read)
 #pragma unroll
         for (int u = 0; u < UPW; ++u) {
-          const Frag<CD> vf = tile_cols<CD>(tile + (EXACT ? u : min(u, nu - 1)) * unit_bytes, sl, lane);
+          const Frag<CD> vf = frag_cols<CD, 32>(tile + (EXACT ? u : min(u, nu - 1)) * unit_bytes, 16 * sl, 0, lane);
 #pragma unroll
           for (int n = 0; n < TP; ++n) o[u] = mma32<CD>(vf, pf[n], o[u]);
         }
