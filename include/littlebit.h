@@ -477,6 +477,9 @@ lb_status lb_dual_svid(const void* W, lb_dtype w_dtype, int64_t d_out, int64_t d
    position 0, past the table's max_pages page_size, or on a page outside [0, n_pages)) is not written
    and not seen, and the places of the others do not depend on it; rows behind cu[n_seq] are neither read nor written.  A place
    named twice in one append holds parts of either token.
+   This form fits models whose heads share one rotary key apart from the projected ones (or have none).  Where the whole
+   projected key of every head is turned by its position (as in the Llama models) a turn stands between U_k and the
+   scores and nothing can be absorbed: turn the expanded keys with lb_rotate and use lb_attention_forward.
    2 r + d_rope <= 1536, d_rope even and <= 256, n_pages page_size < 2^31 and
    max_pages page_size <= 2^30 (LB_ERR_SHAPE); data may be larger than 2^31
    elements and is 16-byte aligned. */
@@ -584,7 +587,8 @@ lb_status lb_attention_forward(const lb_attention* a, void* o, float* lse, hipSt
    d_rope], summed over all heads (NULL if d_rope is 0); all of dtype, written,
    not accumulated, rounded once from fp32 sums.  o and lse are the forward's.
    P and dS are rounded to dtype for their products (dS for dq of heads up to 128
-   wide to two terms of it).  Gradients of grouped heads
+   wide to two terms of it; f16: times powers of two, dS's by the largest |dS| of each query for dq and of
+   each key for dk, so that neither its size nor other rows' cost digits, P's 2^14, for digits down to 2^-28).  Gradients of grouped heads
    are summed in a fixed order: repeated calls give the same bits.  No output may
    overlap an input, another output or the workspace (LB_ERR_ARG; parts of one buffer that
    interleave by their strides are apart).  If H is 0 nothing is written.  workspace: 256-byte

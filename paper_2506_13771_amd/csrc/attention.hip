@@ -9,9 +9,10 @@
 // pair of query and key) and, beside them, by the softmax's vector instructions: two
 // waves a SIMD, so that one's run beside the other's products.
 //
-// Measured (7B heads, 128 + 64 wide keys, 128 wide values, bf16): four prompts of 8192 tokens 241 us, 750
-// TFLOP/s of the seen pairs (a large library product reaches 1120), the matrix cores busy 44%
-// of the CUs' cycles (masked and padded pairs included); 777 tokens of 64 grouped heads in f16 18 us.
+// Measured (7B heads, 128 + 64 wide keys, 128 wide values, bf16): four prompts of 8192 tokens 231 us a call
+// (249 to 259 under the profiler), 780 TFLOP/s of the seen pairs (a large library product reaches 1120), the
+// matrix cores busy 44% of the CUs' cycles (masked and padded pairs included); 777 tokens of 64
+// grouped heads in f16 17.4 us.
 #include "attn.h"
 #include "attn_common.h"
 
@@ -279,9 +280,11 @@ hipError_t fwd_launch(FwdArgs& f, hipStream_t stream) {
   const int seqs = f.a.cu_q ? f.a.n_seq : 0;
   f.n_tiles = (f.a.Tq + kWideRows - 1) / kWideRows + seqs;
   // (16-bit rows that fit no 16-byte loads take the other form, whose loads go through registers.)
-  // us, this form against the other (7B heads, bf16): 96 workgroups (256 rows) 13.1 against 10.8, 160
-  // (512) 20.8 against 23.1, 192 (4 x 512) 9.9 against 16.0; fp32, 64 wide: 72 91.9 against 34.2, 136
-  // 182 against 79
+  // us, this form against the other.  bf16, 7B heads: 96 workgroups (256 rows) 13.2 against 11.4, 160 (512) 19.9
+  // against 23.7, 192 (4 x 128) 11.4 against 17.4; 64 wide: 160 13.0 against 10.3, 192 7.4 against 7.6, 280 9.6 against
+  // 16.1.  fp32, 64 wide: 272 185 against 118, 408 132 against 101, 544 233 against 212, 1056 347 against 418; 128
+  // wide: 272 314 against 240, 408 315 against 359 and 167 against 210, 600 (3 x 2048) 589 against 553.  (Heads of up to 64
+  // columns would cross later: one limit for all widths costs them up to a quarter in between.)
   if (wide_groups(f.a.Tq, seqs, f.a.H) >= (DT == kDtF32 ? 400 : 128) && (f.vec || DT == kDtF32)) return fwd_launch_form<DT, KC, VT, true>(f, stream);
   f.n_tiles = (f.a.Tq + 31) / 32 + seqs;
   return fwd_launch_form<DT, KC, VT, false>(f, stream);

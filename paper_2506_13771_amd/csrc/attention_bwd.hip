@@ -7,7 +7,7 @@
 // rounding of the results themselves, so a gradient is off by about sqrt(2) of its own rounding
 // (measured 1.41 to 1.45).  dQ adds what D has from the rounded O (up to 1.5), so its dS enters in two
 // terms (1.00 to 1.03 then) for heads up to 128 wide; wider ones (1.45 at 192) have no registers
-// left and would pay 17% of their kernel (217 -> 254 us of 2 x 2048 tokens of 7B heads).
+// left and would pay 17% of their kernel (of 2 x 2048 tokens of 7B heads).
 //
 // Two kernels (queries, then keys), each forming S and dO V^T anew, so that every gradient is summed by
 // one owner in a fixed order (no atomics on values): one owns 128 keys of a key head,
@@ -17,8 +17,9 @@
 //
 // Bound by the matrix cores (4 dk + 4 dv operations a pair of query and key in the keys' kernel,
 // 4 dk + 2 dv in the queries') and by what a wave does between them.  Measured (two sequences of
-// 2048 tokens, 7B heads, 128 + 64 wide keys, bf16): queries 203 to 228 us, keys 341 to 370 us; with
-// the forward (126 to 142 us) about 450 TFLOP/s of the least work.  The matrix cores are busy
+// 2048 tokens, 7B heads, 128 + 64 wide keys, bf16, medians after 20 calls): queries 184 us, keys 278 us; with
+// the forward (115 us) 553 TFLOP/s of the least work.  (The first calls on a card at rest are slower:
+// 211, 341 and 133 us.)  The matrix cores are busy
 // 48 and 30% of the CUs' cycles: the keys' wave holds so many operands and sums that one fits
 // a SIMD, and nothing runs beside its loads and exponentials (of 7600 cycles of a step 2200
 // issue loads, 2700 are scores and exponentials, 1900 the last products).  Two waves a
@@ -596,12 +597,15 @@ hipError_t bwd_one(const BwdArgs& f, int T, const int32_t* cu, int heads, hipStr
 template <int DT, int KC, int VT, bool QUERIES>
 hipError_t bwd_form(const BwdArgs& f, int T, const int32_t* cu, int heads, hipStream_t stream) {
   if (T == 0) return hipSuccess;
-  // us of the whole backward with this form of the queries' kernel, and of the keys', against the
-  // other (7B heads, bf16): 160 workgroups (512 rows) 85 against 70, 91 against 85; 192 (4 x 512) 51 against
-  // 51, 49 against 51; 224 (768) 109 against 107, 103 against 109; 288 (1024) 141 against 154, 118 against
-  // 141; fp32, 64 wide, 136 (2048): 360 against 223, 543 against 360.  Four queries' heads a key head: 136
-  // 422 against 257 for the keys.  (The widest fp32 heads' 128 rows do not fit.  16-bit rows that fit
-  // no 16-byte loads take the other form.)
+  // us, 128 rows a workgroup against the other form.  bf16, 7B heads, the queries' kernel: 160 workgroups (512 rows)
+  // 41.2 against 29.8, 192 (4 x 128) 20.4 against 20.4, 224 (768) 41.3 against 41.7, 272 (2048) 79.6 against 75.0, 280 (4 x
+  // 256) 28.4 against 42.4; the keys': 160 39.8 against 35.2, 192 24.4 against 27.7, 224 50.8 against 57.0, 280 31.2
+  // against 52.9, four queries' heads a key head 264 362 against 377.  fp32, 64 wide, queries: 272 251 against 166, 408
+  // 304 against 237, 544 327 against 302, 1056 520 against 594; keys: 272 305 against 191, 408 379 against 262, 544 408
+  // against 340; 128 wide, queries: 272 423 against 336, 408 425 against 488; keys: 272 546 against 375, 408 553 against 558,
+  // 544 601 against 734.  (Heads of up to 64 columns would cross later, above all the keys' with grouped heads: 16-bit 264 260
+  // against 139.  The widest fp32 heads' 128 rows do not fit.  16-bit rows that fit no 16-byte loads
+  // take the other form.)
   if constexpr (lds_of<DT, KC, VT, false>(!QUERIES) <= kLdsMax) {
     if (wide_groups(T, cu ? f.a.n_seq : 0, heads) < (DT == kDtF32 ? 400 : 210) || (DT != kDtF32 && !f.vec))
       return bwd_one<DT, KC, VT, QUERIES, false>(f, T, cu, heads, stream);

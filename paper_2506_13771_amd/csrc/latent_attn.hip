@@ -21,9 +21,9 @@
 // wider rows are cut into four waves' columns, whose scores are added through LDS each step.
 //
 // Measured (7B heads, 2 r + d_rope = 288, bf16, us of absorb + split + join): 32 sequences of 2048 to
-// 16384 tokens 7.8 + 39 + 10.8 (129 MB: 3.3 TB/s over all of split, of which the first loads
-// and the last sums are 11 us, and about what a large copy moves, 5.1, in between); one of 4096 tokens 6.0 + 11.9 + 7.5, a
-// chain of dependent loads; 1440 columns, 8 sequences of 1000 to 4000: 9.4 + 36 + 17.6.
+// 16384 tokens 7.8 + 38.3 + 10.8 (129 MB: 3.3 TB/s over all of split, of which the first loads
+// and the last sums are 11 us, and about what a large copy moves, 5.1, in between); one of 4096 tokens 5.8 + 12.0 + 7.0, a
+// chain of dependent loads; 1440 columns, 8 sequences of 1000 to 4000: 9.0 + 36 + 17.8.
 #include "attn.h"
 #include "attn_common.h"
 #include "latent_map.h"

@@ -6,8 +6,8 @@
 //
 // Both are bound by the bytes they move, and small calls by their launch and the loads
 // that follow one another (prefix sums, length, page, row).  Measured: 8192 tokens x 32 heads x
-// 64 bf16 values 12.9 us, 5.2 TB/s, what a large copy reaches (5.1); 5 fp32 rows 1.8 us; the append of
-// 64 single tokens 5.6 us, of 8 prompts with 7000 tokens (fp32 latents, r = 144, to f16) 10 us.
+// 64 bf16 values 12.7 us, 5.3 TB/s, what a large copy reaches (5.1); 5 fp32 rows 1.7 us; the append of
+// 64 single tokens 5.4 us, of 8 prompts with 7000 tokens (fp32 latents, r = 144, to f16) 10 us.
 #include "attn.h"
 #include "attn_common.h"
 
